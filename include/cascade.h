@@ -450,6 +450,165 @@ cascade_status_t cascade_decode_step_rope(cascade_plan_t* plan, int32_t batch, i
                                           int32_t n_positions, void* o_out, cascade_strides_t o_strides, float* lse_out,
                                           void* workspace, size_t workspace_bytes, void* stream);
 
+/* ---------------------------------------------------------------------------------------------------------------------
+ * Paged caches.  A server holds the K/V rows of many sequences, of lengths that nobody knows beforehand, in pages of one pool.
+ * (The paper's nodes keep the rows of their shard, "Caching" in the appendix on cost optimizations; it does not say how they
+ * lay them out.  A party's pool holds the rows of its own shards, and its calls below return partials like any other.)
+ *
+ * What the calls share:
+ *  - k_pages, v_pages  DEVICE [n_pages][page_size][n_kv_heads][head_dim] with strides (batch: from page to page, token: from row to
+ *                      row of a page, head), so pages may be laid out row by row or head by head; page_size a multiple of 16
+ *  - page_table        DEVICE int32, row b (table_stride apart) the ids of the pages of sequence b, of which max_pages may be read;
+ *                      row y of its cache is row y % page_size of page page_table[b][y / page_size].  Entries past the last page
+ *                      that the length needs may hold anything
+ *  - row_start         DEVICE int32 [batch + 1]: the new rows of sequence b are rows row_start[b] .. row_start[b + 1] - 1 of
+ *                      tensors [n_rows][heads][head_dim] (strides.batch is not used).  Rows before the first and behind the last
+ *                      sequence are padding: outputs leave them as they were
+ *  - kv_len            DEVICE int32 [batch]: rows in the cache of sequence b, its new rows counted
+ * Lengths, row starts and tables are read on the device when the call runs, so a captured graph follows them.  What they say is
+ * checked there before it forms an address.  A bad row_start counts as no rows, a bad length as the nearest good one, a bad page
+ * id as page 0 (nothing is written to it); the first is kept for cascade_paged_status, and the outputs of its sequence are then
+ * not to be used.
+ * Two calls that write the same pages, or pages that the other reads, have to be ordered by the caller.
+ */
+
+/* Reads and clears what the paged calls on the current device have reported (SYNCHRONISES the device).  *out_code: 0, a code of
+ * 121 on for a bad index (BAD_MAP; the message names it and where it stood), or that of a bounded wait that gave up (TIMEOUT).
+ * After a wait has given up, later tensor-core calls on paged caches write nothing until this has been called. */
+cascade_status_t cascade_paged_status(int32_t* out_code);
+
+/*
+ * cascade_rope_table_scaled -- cascade_rope_table for angles stretched to longer contexts: theta_i = base^(-2 i / rot_dim), i <
+ * rot_dim / 2, then by `kind`
+ *   CASCADE_ROPE_NONE    as it is
+ *   CASCADE_ROPE_LINEAR  theta / factor
+ *   CASCADE_ROPE_BASE    base * factor^(rot_dim / (rot_dim - 2)) in the place of base (rot_dim above 2)
+ *   CASCADE_ROPE_BANDS   by the turns t = original_positions theta / (2 pi): theta for t >= high, theta / factor for t <= low, and
+ *                        between them mixed with weight (t - low) / (high - low) of theta
+ *   CASCADE_ROPE_RAMP    by the dimension: D(t) = rot_dim ln(original_positions / (2 pi t)) / (2 ln base) turns t times; theta up
+ *                        to a = max(0, floor D(high)), theta / factor from b = min(rot_dim - 1, ceil D(low)) on, mixed with
+ *                        weight (i - a) / (b - a) of the latter between them
+ * cos and sin are multiplied by `attention`; 0 stands for 0.1 ln(factor) + 1 with RAMP and 1 otherwise.
+ *   table  DEVICE fp32 [n_positions][rot_dim / 2][2], 16-byte aligned.  Angles are formed in fp64.
+ * Errors: INVALID_ARG (sizes, an odd rot_dim, base <= 1, factor < 1, not 0 < low < high or original_positions <= 0 where they are
+ * used), CUDA.
+ */
+enum { CASCADE_ROPE_NONE = 0, CASCADE_ROPE_LINEAR = 1, CASCADE_ROPE_BASE = 2, CASCADE_ROPE_BANDS = 3, CASCADE_ROPE_RAMP = 4 };
+cascade_status_t cascade_rope_table_scaled(int32_t n_positions, int32_t rot_dim, double base, int32_t kind, double factor,
+                                           double original_positions, double low, double high, double attention,
+                                           float* table, void* stream);
+
+/*
+ * cascade_rope_rows -- the rotary step of the Pre-Pass algorithm for rows that stand anywhere: row r by the table row of
+ * positions[r].  Only the first rot_dim columns are turned, the others pass through:
+ *   interleaved = 0   pairs (i, i + rot_dim / 2)        interleaved = 1   pairs (2 i, 2 i + 1)         i < rot_dim / 2
+ * in fp32, rounded once to `dtype`.
+ *   x, y        DEVICE [n_rows][n_heads][head_dim] with strides (batch unused); y may be x.  head_dim 64 or 128
+ *   positions   DEVICE int32 [n_rows]; a negative one marks a padded row, whose y stays as it was
+ *   rope_table  DEVICE fp32 [n_positions][rot_dim / 2][2]; rot_dim a multiple of 16, at most head_dim
+ * A position past the table is reported to cascade_paged_status and its row left as it was.
+ * Errors: INVALID_ARG, UNSUPPORTED (dtype, head_dim, rot_dim), CUDA.
+ */
+cascade_status_t cascade_rope_rows(cascade_dtype_t dtype, int32_t n_rows, int32_t n_heads, int32_t head_dim, int32_t rot_dim,
+                                   int32_t interleaved, const void* x, cascade_strides_t x_strides, const int32_t* positions,
+                                   const float* rope_table, int32_t n_positions, void* y, cascade_strides_t y_strides,
+                                   void* stream);
+
+/*
+ * cascade_paged_append -- the new rows of a batch go to the pages of their sequences, in one launch: row i of the n of sequence b
+ * becomes row y = kv_len[b] - n + i of its cache.  With rope_table k is turned on the way as by cascade_rope_rows (rot_dim,
+ * interleaved), and so are the queries: q_out = R q.
+ *   k, v       DEVICE [n_rows][n_kv_heads][head_dim] with strides;  q, q_out  DEVICE [n_rows][n_heads][head_dim] or both NULL;
+ *              q_out may be q
+ *   positions  DEVICE int32 [n_rows] or NULL: y itself.  (A party that holds some of the tokens gives the original ones.)
+ *   rope_table NULL: rows are taken as they are
+ * A row whose place, page or position is bad is reported and not written.  Errors: INVALID_ARG, UNSUPPORTED, CUDA.
+ */
+cascade_status_t cascade_paged_append(cascade_dtype_t dtype, int32_t batch, int32_t n_rows, int32_t n_heads,
+                                      int32_t n_kv_heads, int32_t head_dim, const void* q, cascade_strides_t q_strides,
+                                      void* q_out, cascade_strides_t q_out_strides, const void* k,
+                                      cascade_strides_t k_strides, const void* v, cascade_strides_t v_strides,
+                                      const int32_t* positions, const float* rope_table, int32_t n_positions,
+                                      int32_t rot_dim, int32_t interleaved, void* k_pages, cascade_strides_t k_page_strides,
+                                      void* v_pages, cascade_strides_t v_page_strides, int32_t n_pages, int32_t page_size,
+                                      const int32_t* page_table, int64_t table_stride, int32_t max_pages,
+                                      const int32_t* row_start, const int32_t* kv_len, void* stream);
+
+/*
+ * cascade_attn_paged -- the Attention-Pass and Post-Pass algorithms for the new rows of a ragged batch over their paged caches:
+ * chunks of prompts, single tokens and drafts side by side, or the rows of a decoder over an encoder's states of another length.
+ *   q, o_out   DEVICE [n_rows][n_heads][head_dim] with strides;  lse_out  optional fp32 [n_rows][n_heads]
+ *   causal     1: row i of the n of sequence b sees the cache rows y <= kv_len[b] - n + i;  0: all kv_len[b]
+ *   visible    DEVICE int32 [n_rows] or NULL: the number of cache rows that a row sees instead (at most kv_len[b]); for a party
+ *              whose pool holds the rows of a shard, VIS of its plan (cascade_shard_plan_resident)
+ *   max_rows   no sequence has more rows; goes into the choice of kernels only, but a sequence with more is reported and may be
+ *              left as it was
+ * A row that sees nothing yields zeros and lse = -inf.  (o_out, lse_out, 1) of one party is a partial (u, m, l) for cascade_merge
+ * with those of others.  Rows of the cache that no length reaches may hold anything, NaN included.
+ * bf16 and fp32, head_dim 64 and 128, n_heads a multiple of n_kv_heads.  bf16 runs on the tensor cores; K and V row starts must be
+ * 16-byte aligned.  scale positive and finite.
+ *   workspace  cascade_attn_paged_workspace_bytes(...) bytes, 256-byte aligned; overwritten by every call, so calls that may run at
+ *              the same time need one each
+ * Errors: INVALID_ARG, UNSUPPORTED, WORKSPACE, CUDA.
+ */
+cascade_status_t cascade_attn_paged(cascade_dtype_t dtype, int32_t batch, int32_t n_rows, int32_t max_rows, int32_t n_heads,
+                                    int32_t n_kv_heads, int32_t head_dim, float scale, int32_t causal, const void* q,
+                                    cascade_strides_t q_strides, const void* k_pages, cascade_strides_t k_page_strides,
+                                    const void* v_pages, cascade_strides_t v_page_strides, int32_t n_pages,
+                                    int32_t page_size, const int32_t* page_table, int64_t table_stride, int32_t max_pages,
+                                    const int32_t* row_start, const int32_t* kv_len, const int32_t* visible, void* o_out,
+                                    cascade_strides_t o_strides, float* lse_out, void* workspace, size_t workspace_bytes,
+                                    void* stream);
+cascade_status_t cascade_attn_paged_workspace_bytes(cascade_dtype_t dtype, int32_t batch, int32_t n_rows, int32_t max_rows,
+                                                    int32_t n_heads, int32_t n_kv_heads, int32_t head_dim,
+                                                    int32_t page_size, int32_t max_pages, size_t* out_bytes);
+
+/*
+ * cascade_pages_fork -- one step of the page tables, on the device: sequence i of the new state continues sequence source[i] of the
+ * old one (-1: none, the place is emptied; the same source any number of times) and gets room for add[i] more rows.
+ * A page is held by every sequence whose length reaches it, and free when none holds it.  Pages are shared as they are; a sequence
+ * that goes on writing a partly filled page which others hold, too, gets a copy of its own, except the first of them where all of
+ * its holders do.  New pages are the free ones with the lowest ids, in the order of the sequences (the copy first).
+ *   table_in, kv_len_in    DEVICE int32 [n_seqs][width], [n_seqs]: the old state;  source, add  DEVICE int32 [n_seqs]
+ *   table_out, kv_len_out  the new one (kv_len = old + add); entries past the last page -1.  May not overlap the old one
+ *   refs      DEVICE int32 [n_pages], written: holders of every page
+ *   copies    DEVICE int32 [n_seqs][2], written: (from, to) for cascade_pages_copy, before the new rows are appended; or (-1, -1)
+ *   report    DEVICE int32 [4], written: pages lacking; sequences that the table is too narrow for; bad entries (a source, a
+ *             length, a page id, a negative add); pages left free.  Unless the first three are 0 nothing is done: the new state is
+ *             the old one
+ * One launch, no atomics whose order matters.  n_seqs at most 8192.  Errors: INVALID_ARG, UNSUPPORTED, CUDA.
+ */
+cascade_status_t cascade_pages_fork(int32_t n_seqs, int32_t width, int32_t n_pages, int32_t page_size,
+                                    const int32_t* table_in, const int32_t* kv_len_in, const int32_t* source,
+                                    const int32_t* add, int32_t* table_out, int32_t* kv_len_out, int32_t* refs,
+                                    int32_t* copies, int32_t* report, void* stream);
+
+/*
+ * cascade_pages_compact -- moves the held pages together at the front of the pool: of n_live held pages, those from id n_live on go,
+ * in order, to the free ids below it; the others stay.  (Fewest moves, and no page is both moved and moved to.)
+ *   table_out  the table with the new ids, entries past the last page -1; may not overlap table_in
+ *   refs       as cascade_pages_fork, by the new ids
+ *   moves      DEVICE int32 [n_pages / 2][2], written: (from, to) for cascade_pages_copy, then (-1, -1)
+ *   report     DEVICE int32 [4], written: n_live; moves; bad entries (then nothing is moved); free pages
+ * Errors: INVALID_ARG, CUDA.
+ */
+cascade_status_t cascade_pages_compact(int32_t n_seqs, int32_t width, int32_t n_pages, int32_t page_size,
+                                       const int32_t* table_in, const int32_t* kv_len, int32_t* table_out, int32_t* refs,
+                                       int32_t* moves, int32_t* report, void* stream);
+
+/*
+ * cascade_pages_copy -- copies page pairs[j][0] over page pairs[j][1] in every pool (K and V of every layer), in one launch; pairs
+ * with a -1 are skipped, ids past n_pages reported to cascade_paged_status.  No page may be copied to twice, or both from and to
+ * (what it then holds is not defined).
+ *   pools        HOST array of n_pools (at most 256) DEVICE pointers, 16-byte aligned
+ *   page_strides HOST int64 [n_pools]: bytes from page to page, at least page_bytes
+ *   page_bytes   bytes of a page, which is contiguous; a multiple of 16
+ *   pairs        DEVICE int32 [n_pairs][2]
+ * Errors: INVALID_ARG, UNSUPPORTED (more pools), CUDA.
+ */
+cascade_status_t cascade_pages_copy(int32_t n_pools, void* const* pools, const int64_t* page_strides, int64_t page_bytes,
+                                    int32_t n_pages, const int32_t* pairs, int32_t n_pairs, void* stream);
+
 enum {
   CASCADE_CALL_PARTIALS = 0,
   CASCADE_CALL_SHARDED = 1,

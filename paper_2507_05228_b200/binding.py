@@ -35,6 +35,8 @@ EXPORTS = [
     "cascade_cdelta_shard_map", "cascade_msplit_shard_map", "cascade_index_set_gaps", "cascade_kl_gaps",
     "cascade_attn_sharded_host", "cascade_plan_advance", "cascade_shard_plan_resident",
     "cascade_shard_plan_resident_host", "cascade_rope_apply", "cascade_decode_step_rope", "cascade_merge_peers",
+    "cascade_paged_status", "cascade_rope_table_scaled", "cascade_rope_rows", "cascade_paged_append", "cascade_attn_paged",
+    "cascade_attn_paged_workspace_bytes", "cascade_pages_fork", "cascade_pages_compact", "cascade_pages_copy",
 ]
 
 
@@ -102,6 +104,18 @@ def lib() -> ctypes.CDLL:
         L.cascade_kl_gaps.argtypes = [i32, vp, vp, i32, vp]
         L.cascade_attn_sharded_host.argtypes = [vp, i32, i32, i32, i32, i32, f32, vp, vp, vp, vp, vp, ctypes.c_size_t, vp]
         L.cascade_plan_advance.argtypes = [vp, i32, vp]
+        L.cascade_paged_status.argtypes = [pi32]
+        dbl = ctypes.c_double
+        L.cascade_rope_table_scaled.argtypes = [i32, i32, dbl, i32, dbl, dbl, dbl, dbl, dbl, vp, vp]
+        L.cascade_rope_rows.argtypes = [i32, i32, i32, i32, i32, i32, vp, Strides, vp, vp, i32, vp, Strides, vp]
+        L.cascade_paged_append.argtypes = [i32, i32, i32, i32, i32, i32, vp, Strides, vp, Strides, vp, Strides, vp, Strides, vp, vp,
+                                           i32, i32, i32, vp, Strides, vp, Strides, i32, i32, vp, i64, i32, vp, vp, vp]
+        L.cascade_attn_paged.argtypes = [i32, i32, i32, i32, i32, i32, i32, f32, i32, vp, Strides, vp, Strides, vp, Strides, i32, i32,
+                                         vp, i64, i32, vp, vp, vp, vp, Strides, vp, vp, ctypes.c_size_t, vp]
+        L.cascade_attn_paged_workspace_bytes.argtypes = [i32] * 9 + [ctypes.POINTER(ctypes.c_size_t)]
+        L.cascade_pages_fork.argtypes = [i32, i32, i32, i32, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp]
+        L.cascade_pages_compact.argtypes = [i32, i32, i32, i32, vp, vp, vp, vp, vp, vp, vp]
+        L.cascade_pages_copy.argtypes = [i32, vp, vp, i64, i32, vp, i32, vp]
         L.cascade_kernel_timing_begin.argtypes = []
         L.cascade_kernel_timing_end.argtypes = [ctypes.POINTER(ctypes.c_double), ctypes.POINTER(i64)]
         for name in EXPORTS:
@@ -372,6 +386,78 @@ def cascade_attn_decode_static(plan: Plan, q: torch.Tensor, k: torch.Tensor, v: 
     scratch memory.  Only the output tensors are created here; the C call itself allocates nothing.
     Returns (o [B, 1, H, 128], lse or None)."""
     return _native().attn_decode_static(plan.handle, q, k, v, scale, out, want_lse)
+
+
+ROPE_KINDS = {"none": 0, "linear": 1, "base": 2, "bands": 3, "ramp": 4}
+
+
+def cascade_rope_table_scaled(n_positions: int, rot_dim: int, base: float, kind: str = "none", factor: float = 1.0,
+                              original_positions: float = 0.0, low: float = 1.0, high: float = 4.0, attention: float = 0.0,
+                              device="cuda") -> torch.Tensor:
+    """Positional table fp32 [n_positions, rot_dim/2, 2] with angles stretched for a context `factor` times as long: kind "none",
+    "linear", "base", "bands" or "ramp" (include/cascade.h has the formulas); attention 0: the kind's own factor on cos and sin."""
+    if kind not in ROPE_KINDS:
+        raise CascadeError(1, f"cascade_rope_table_scaled: unknown kind {kind!r}")
+    table = torch.empty((max(int(n_positions), 0), rot_dim // 2, 2), dtype=torch.float32, device=device)
+    _check(lib().cascade_rope_table_scaled(n_positions, rot_dim, float(base), ROPE_KINDS[kind], float(factor),
+                                           float(original_positions), float(low), float(high), float(attention),
+                                           table.data_ptr(), _stream()))
+    return table
+
+
+def cascade_rope_rows(x: torch.Tensor, positions: torch.Tensor, rope_table: torch.Tensor, interleaved: bool = False,
+                      out=None) -> torch.Tensor:
+    """x [rows, heads, d] with its first rot_dim = 2 * rope_table.shape[1] columns turned by the table rows positions[r] (int32,
+    on the GPU; negative: out keeps what it holds there).  Pairs (i, i + rot_dim/2), or (2i, 2i+1) if interleaved.  out may be x."""
+    return _native().rope_rows(x, positions, rope_table, interleaved, out)
+
+
+def cascade_paged_append(k: torch.Tensor, v: torch.Tensor, k_pages: torch.Tensor, v_pages: torch.Tensor, page_table: torch.Tensor,
+                         row_start: torch.Tensor, kv_len: torch.Tensor, q: Optional[torch.Tensor] = None, positions=None,
+                         rope_table=None, interleaved: bool = False, q_out=None):
+    """The new rows k, v [rows, kv_heads, d] go to the pages [n_pages, page_size, kv_heads, d] of their sequences: the rows
+    row_start[b] .. row_start[b+1]-1 become the last ones of the kv_len[b] rows of sequence b (page_table int32 [batch, pages]).
+    With rope_table k is turned by its place in the cache, or by positions [rows], and q [rows, heads, d] with it: returns q_out
+    (which may be q), or None without q."""
+    return _native().paged_append(k, v, k_pages, v_pages, page_table, row_start, kv_len, q, positions, rope_table, interleaved, q_out)
+
+
+def cascade_attn_paged(q: torch.Tensor, k_pages: torch.Tensor, v_pages: torch.Tensor, page_table: torch.Tensor,
+                       row_start: torch.Tensor, kv_len: torch.Tensor, scale: float, causal: bool = True, visible=None,
+                       max_rows: Optional[int] = None, out=None, want_lse: bool = True, workspace=None):
+    """Attention of the new rows q [rows, heads, d] of a ragged batch over their paged caches (see cascade_paged_append for the
+    other tensors).  causal: row i of the n of sequence b sees its cache up to row kv_len[b] - n + i; otherwise all of it; or the
+    first visible[r] rows.  max_rows: no sequence has more new rows (default: all there are).  Returns (o, lse [rows, heads] or
+    None); rows behind the last sequence are left as they are."""
+    return _native().attn_paged(q, k_pages, v_pages, page_table, row_start, kv_len, scale, causal, visible, max_rows, out, want_lse,
+                                workspace)
+
+
+def cascade_pages_fork(page_table: torch.Tensor, kv_len: torch.Tensor, source: torch.Tensor, add: torch.Tensor, n_pages: int,
+                       page_size: int, out=None):
+    """One step of the page tables: sequence i continues sequence source[i] (-1: none) and gets room for add[i] rows.  Returns
+    (page_table, kv_len, refs [n_pages], copies [sequences, 2], report [4]); the copies go to cascade_pages_copy.  Unless
+    report[:3] (pages lacking, tables too narrow, bad entries) is 0, nothing is done.  out: a tuple of the five tensors."""
+    return _native().pages_fork(page_table, kv_len, source, add, n_pages, page_size, out)
+
+
+def cascade_pages_compact(page_table: torch.Tensor, kv_len: torch.Tensor, n_pages: int, page_size: int, out=None):
+    """Moves the held pages together at the front of the pool.  Returns (page_table, refs, moves [n_pages // 2, 2], report [4] =
+    (held pages, moves, bad entries, free pages)); the moves go to cascade_pages_copy."""
+    return _native().pages_compact(page_table, kv_len, n_pages, page_size, out)
+
+
+def cascade_pages_copy(pools, pairs: torch.Tensor) -> None:
+    """Copies page pairs[j, 0] over page pairs[j, 1] in every pool [n_pages, ...] of the list (pages dense, of one size); pairs with
+    a -1 are skipped."""
+    _native().pages_copy(pools, pairs)
+
+
+def cascade_paged_status() -> int:
+    """Reads and clears what the paged calls on the current device have reported (synchronises): 0, or raises CascadeError."""
+    code = ctypes.c_int32()
+    _check(lib().cascade_paged_status(ctypes.byref(code)))
+    return code.value
 
 
 def _np_ptr(a: np.ndarray):

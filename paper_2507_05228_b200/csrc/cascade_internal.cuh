@@ -43,6 +43,17 @@ struct Strides {
   int64_t batch, token, head;
 };
 
+// A paged cache and the ragged rows of a call on it (cascade_attn_paged); helpers in paged.cuh.
+struct PagedDev {
+  const int32_t* table;  // [batch][table_stride]: ids of the pages of each sequence
+  int64_t table_stride;
+  const int32_t *row_start, *kv_len;  // [batch + 1], [batch]
+  const int32_t* visible;             // [n_rows] or null: cache rows that a row sees
+  int32_t* status;                    // see PagedStatus
+  int32_t batch, n_rows, n_pages, max_pages, page_size;
+  int32_t least, most;  // sequences of least .. most rows are this kernel's
+};
+
 struct AttnParams {
   PlanDev plan;
   const void* q;
@@ -66,6 +77,10 @@ struct AttnParams {
   // rope[position * 64 + i] = (cos, sin) of position * theta_i; null = rows are used as given.  A query row sits at
   // position q_pos_offset + token, a key row at its token index.
   const float2* rope;
+  // Paged calls: K and V are pages (ks.batch, vs.batch: from page to page; token: from row to row of a page), q and o_out rows of
+  // all sequences one after another.  Of `plan` only causal and status are set.
+  PagedDev paged;
+  int32_t key_parts;  // paged ALU kernel: CTAs that share the keys of a tile; more than one: partials [key_parts][n_rows][H]
 };
 
 // Debug build (-DCASCADE_DEBUG, libcascade_b200_debug.so): every row index that a kernel reads out of a plan array
@@ -274,5 +289,49 @@ cudaError_t launch_plan_fill(const PlanDev& d, const void* q_src, const void* kv
 cudaError_t launch_plan_advance(const PlanDev& d, int32_t q_pos_offset, cudaStream_t stream);
 cudaError_t launch_merge(const MergeParams& p, cascade_dtype_t dtype, cudaStream_t stream);
 cudaError_t launch_merge_peers(const MergePeersParams& p, cascade_dtype_t dtype, cudaStream_t stream);
+
+// ---- paged caches
+// The device words that paged calls report to, of the current device (part of the module, nothing is allocated); null on error.
+int32_t* paged_status_words();
+// fp32, and bf16 where nothing else takes it: CTAs that share the keys of a tile, bytes of the partials they leave, the launch
+int paged_alu_parts(const AttnParams& p);
+size_t paged_alu_ws_bytes(const AttnParams& p);
+cudaError_t launch_paged_alu(AttnParams p, cascade_dtype_t dtype, void* workspace, cudaStream_t stream);
+
+// Rows turned by their positions and, with pages, appended (cascade_rope_rows, cascade_paged_append)
+struct RopeRowsParams {
+  const void *q, *k, *v;  // [n_rows][heads][d]; q or k and v may be absent
+  void *q_out, *k_out, *v_out;  // k_out, v_out: pages
+  Strides qs, qos, ks, vs, kos, vos;  // of pages: batch = from page to page, token = from row to row
+  const float2* rope;  // [n_positions][rot / 2], null: rows are taken as they are
+  const int32_t* positions;  // [n_rows]; null: the row of the cache
+  PagedDev paged;  // append only
+  int32_t n_rows, H, Hkv, d, rot, interleaved, n_positions;
+};
+cudaError_t launch_rope_rows(const RopeRowsParams& p, cascade_dtype_t dtype, cudaStream_t stream);
+struct RopeScaling {
+  int32_t kind;
+  double base, factor, original, low, high, attention;
+};
+cudaError_t launch_rope_table_scaled(int32_t n_positions, int32_t rot, const RopeScaling& s, float2* table, cudaStream_t stream);
+
+// Page tables (pages.cu)
+struct PagesParams {
+  const int32_t *table_in, *kv_in, *source, *add;
+  int32_t *table_out, *kv_out, *refs, *pairs, *report;
+  int32_t n_seqs, width, n_pages, page_size, max_pairs;
+};
+cudaError_t launch_pages_fork(const PagesParams& p, cudaStream_t stream);
+cudaError_t launch_pages_compact(const PagesParams& p, cudaStream_t stream);
+constexpr int kMaxPools = 256;
+struct PagesCopyParams {
+  void* pool[kMaxPools];
+  int64_t page_stride[kMaxPools];  // bytes
+  int64_t page_bytes;
+  const int32_t* pairs;  // [n_pairs][2]
+  int32_t* status;
+  int32_t n_pools, n_pairs, n_pages;
+};
+cudaError_t launch_pages_copy(const PagesCopyParams& p, cudaStream_t stream);
 
 }  // namespace cascade

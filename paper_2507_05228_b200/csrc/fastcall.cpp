@@ -9,6 +9,9 @@
 #include <torch/csrc/Exceptions.h>
 #include <torch/csrc/autograd/python_variable.h>
 
+#include <algorithm>
+#include <vector>
+
 #include "cascade.h"
 
 namespace {
@@ -23,6 +26,13 @@ struct Api {
   decltype(&cascade_decode_step_rope) decode_step_rope;
   decltype(&cascade_attn_decode_static) decode_static;
   decltype(&cascade_plan_advance) plan_advance;
+  decltype(&cascade_rope_rows) rope_rows;
+  decltype(&cascade_paged_append) paged_append;
+  decltype(&cascade_attn_paged) attn_paged;
+  decltype(&cascade_attn_paged_workspace_bytes) attn_paged_workspace_bytes;
+  decltype(&cascade_pages_fork) pages_fork;
+  decltype(&cascade_pages_compact) pages_compact;
+  decltype(&cascade_pages_copy) pages_copy;
 };
 Api api;
 PyObject* cascade_error = nullptr;  // CascadeError(status, message)
@@ -319,6 +329,267 @@ PyObject* plan_advance(PyObject* const* a) {
   Py_RETURN_NONE;
 }
 
+// ---------------------------------------------------------------------------------------------------- paged caches
+
+// A tensor of the current device, whose stream the call goes to.
+const at::Tensor& here(PyObject* o) {
+  const at::Tensor& t = tensor(o);
+  if (!t.is_cuda()) raise(PyExc_ValueError, "a tensor on the GPU is expected");
+  if (t.get_device() != c10::cuda::current_device()) raise(PyExc_ValueError, "a tensor is on another device than the current one");
+  return t;
+}
+cascade_strides_t row_strides(const at::Tensor& t) {  // [rows, heads, head_dim]
+  if (t.dim() != 3 || t.stride(2) != 1) raise(PyExc_AssertionError, "expected [rows, heads, head_dim] with contiguous head_dim");
+  return {0, t.stride(0), t.stride(1)};
+}
+cascade_strides_t page_strides(const at::Tensor& t) {
+  if (t.dim() != 4 || t.stride(3) != 1)
+    raise(PyExc_AssertionError, "expected pages [n_pages, page_size, kv_heads, head_dim] with contiguous head_dim");
+  return {t.stride(0), t.stride(1), t.stride(2)};
+}
+void need(bool fine, const char* message) {
+  if (!fine) raise(PyExc_ValueError, message);
+}
+const int32_t* ints(const at::Tensor& t, int64_t n, const char* message) {
+  if (t.scalar_type() != at::kInt || t.dim() != 1 || t.size(0) != n || (n > 1 && t.stride(0) != 1)) raise(PyExc_ValueError, message);
+  return static_cast<const int32_t*>(t.data_ptr());
+}
+const float* rope_table(const at::Tensor& t, int32_t& n_positions, int32_t& rot) {
+  if (t.scalar_type() != at::kFloat || !t.is_contiguous() || t.dim() != 3 || t.size(2) != 2)
+    raise(PyExc_AssertionError, "the positional table is fp32 [positions, rot_dim / 2, 2], contiguous");
+  n_positions = size(t, 0);
+  rot = 2 * size(t, 1);
+  return static_cast<const float*>(t.data_ptr());
+}
+struct Pages {
+  const at::Tensor &k, &v, &table;
+  cascade_strides_t ks, vs;
+  void *kp, *vp;
+  const int32_t *tp, *starts, *len;
+  int64_t table_stride;
+  int32_t n_pages, page_size, Hkv, d, batch, max_pages;
+  Pages(PyObject* k_, PyObject* v_, PyObject* table_, PyObject* starts_, PyObject* len_)
+      : k(here(k_)), v(here(v_)), table(here(table_)), ks(page_strides(k)), vs(page_strides(v)) {
+    need(k.sizes() == v.sizes() && k.scalar_type() == v.scalar_type(), "k_pages and v_pages must be of one shape and type");
+    need(table.scalar_type() == at::kInt && table.dim() == 2 && (table.size(1) <= 1 || table.stride(1) == 1),
+         "the page table is int32 [sequences, pages] with contiguous rows");
+    n_pages = size(k, 0);
+    page_size = size(k, 1);
+    Hkv = size(k, 2);
+    d = size(k, 3);
+    batch = size(table, 0);
+    max_pages = size(table, 1);
+    table_stride = batch > 1 ? table.stride(0) : max_pages;
+    starts = ints(here(starts_), (int64_t)batch + 1, "row_start is int32 [sequences + 1]");
+    len = ints(here(len_), batch, "kv_len is int32 [sequences]");
+    kp = k.data_ptr();
+    vp = v.data_ptr();
+    tp = static_cast<const int32_t*>(table.data_ptr());
+  }
+};
+
+// (x, positions, rope_table, interleaved, out or None) -> out
+PyObject* rope_rows(PyObject* const* a) {
+  const at::Tensor &x = here(a[0]), &positions = here(a[1]), &table = here(a[2]);
+  const cascade_strides_t xs = row_strides(x);
+  const cascade_dtype_t code = dtype_code(x);
+  const int32_t n = size(x, 0), H = size(x, 1), d = size(x, 2);
+  const int32_t* pos = ints(positions, n, "positions is int32 [rows]");
+  int32_t n_positions, rot;
+  const float* tp = rope_table(table, n_positions, rot);
+  const int32_t interleaved = truth(a[3]);
+  const at::Tensor y = a[4] == Py_None ? at::empty_like(x) : here(a[4]);
+  const cascade_strides_t ys = row_strides(y);
+  need(y.sizes() == x.sizes() && y.scalar_type() == x.scalar_type(), "out must be of x's shape and type");
+  if (n > 0) {
+    void *st = stream(), *xp = x.data_ptr(), *yp = y.data_ptr();
+    check(unlocked([&] { return api.rope_rows(code, n, H, d, rot, interleaved, xp, xs, pos, tp, n_positions, yp, ys, st); }));
+  }
+  return wrap(y);
+}
+
+// (k, v, k_pages, v_pages, page_table, row_start, kv_len, q or None, positions or None, rope_table or None, interleaved, q_out or None)
+// -> q_out or None
+PyObject* paged_append(PyObject* const* a) {
+  const at::Tensor &k = here(a[0]), &v = here(a[1]);
+  const Pages g(a[2], a[3], a[4], a[5], a[6]);
+  const cascade_strides_t ks = row_strides(k), vs = row_strides(v);
+  const cascade_dtype_t code = dtype_code(k);
+  const int32_t n = size(k, 0);
+  need(k.sizes() == v.sizes() && size(k, 1) == g.Hkv && size(k, 2) == g.d, "k and v must be [rows, kv_heads, head_dim] of the pages");
+  need(v.scalar_type() == k.scalar_type() && g.k.scalar_type() == k.scalar_type(), "k, v and the pages must be of one type");
+  at::Tensor q, q_out;
+  cascade_strides_t qs = {0, 0, 0}, qos = {0, 0, 0};
+  int32_t H = 0;
+  if (a[7] != Py_None) {
+    q = here(a[7]);
+    qs = row_strides(q);
+    H = size(q, 1);
+    need(size(q, 0) == n && size(q, 2) == g.d && q.scalar_type() == k.scalar_type(), "q must be [rows, heads, head_dim] of k's type");
+    q_out = a[11] == Py_None ? at::empty_like(q) : here(a[11]);
+    qos = row_strides(q_out);
+    need(q_out.sizes() == q.sizes() && q_out.scalar_type() == q.scalar_type(), "q_out must be of q's shape and type");
+  }
+  const int32_t* pos = a[8] == Py_None ? nullptr : ints(here(a[8]), n, "positions is int32 [rows]");
+  int32_t n_positions = 0, rot = 0;
+  const float* tp = a[9] == Py_None ? nullptr : rope_table(here(a[9]), n_positions, rot);
+  const int32_t interleaved = truth(a[10]);
+  if (n > 0) {
+    void *st = stream(), *kp = k.data_ptr(), *vp = v.data_ptr(), *qp = q.defined() ? q.data_ptr() : nullptr,
+         *qop = q.defined() ? q_out.data_ptr() : nullptr;
+    check(unlocked([&] {
+      return api.paged_append(code, g.batch, n, H, g.Hkv, g.d, qp, qs, qop, qos, kp, ks, vp, vs, pos, tp, n_positions, rot, interleaved,
+                              g.kp, g.ks, g.vp, g.vs, g.n_pages, g.page_size, g.tp, g.table_stride, g.max_pages, g.starts, g.len, st);
+    }));
+  }
+  return wrap(q_out);
+}
+
+// (q, k_pages, v_pages, page_table, row_start, kv_len, scale, causal, visible or None, max_rows or None, out or None, want_lse,
+// workspace or None) -> (o, lse or None)
+PyObject* attn_paged(PyObject* const* a) {
+  const at::Tensor& q = here(a[0]);
+  const Pages g(a[1], a[2], a[3], a[4], a[5]);
+  const cascade_strides_t qs = row_strides(q);
+  const cascade_dtype_t code = dtype_code(q);
+  const int32_t n = size(q, 0), H = size(q, 1);
+  need(size(q, 2) == g.d && g.k.scalar_type() == q.scalar_type(), "q and the pages must be of one head_dim and type");
+  const float scale = number(a[6]);
+  const int32_t causal = truth(a[7]);
+  const int32_t* visible = a[8] == Py_None ? nullptr : ints(here(a[8]), n, "visible is int32 [rows]");
+  const int32_t max_rows = a[9] == Py_None ? std::max(n, 1) : (int32_t)integer(a[9]);
+  const at::Tensor o = a[10] == Py_None ? at::empty_like(q) : here(a[10]);
+  const cascade_strides_t os = row_strides(o);
+  need(o.sizes() == q.sizes() && o.scalar_type() == q.scalar_type(), "out must be of q's shape and type");
+  at::Tensor lse;
+  if (truth(a[11])) lse = at::empty({n, H}, q.options().dtype(at::kFloat));
+  if (n > 0) {
+    size_t bytes = 0;
+    check(api.attn_paged_workspace_bytes(code, g.batch, n, max_rows, H, g.Hkv, g.d, g.page_size, g.max_pages, &bytes));
+    Scratch ws;
+    if (bytes > 0) {
+      ws.own = a[12] == Py_None ? at::empty({(int64_t)bytes}, q.options().dtype(at::kByte)) : here(a[12]);
+      ws.ptr = ws.own.data_ptr();
+      ws.bytes = (size_t)ws.own.numel() * ws.own.element_size();
+    }
+    void *st = stream(), *qp = q.data_ptr(), *op = o.data_ptr();
+    float* lp = data_or_null(lse);
+    check(unlocked([&] {
+      return api.attn_paged(code, g.batch, n, max_rows, H, g.Hkv, g.d, scale, causal, qp, qs, g.kp, g.ks, g.vp, g.vs, g.n_pages, g.page_size,
+                            g.tp, g.table_stride, g.max_pages, g.starts, g.len, visible, op, os, lp, ws.ptr, ws.bytes, st);
+    }));
+  }
+  return pair(a[10], o, lse);
+}
+
+at::Tensor like_ints(const at::Tensor& t, at::IntArrayRef shape) { return at::empty(shape, t.options().dtype(at::kInt)); }
+// `out`: a sequence of n tensors for the results, or None
+std::vector<at::Tensor> results(PyObject* out, const at::Tensor& like, std::initializer_list<std::vector<int64_t>> shapes) {
+  std::vector<at::Tensor> r;
+  if (out == Py_None) {
+    for (const auto& s : shapes) r.push_back(like_ints(like, s));
+    return r;
+  }
+  need(PyTuple_Check(out) && PyTuple_GET_SIZE(out) == (Py_ssize_t)shapes.size(), "out: a tuple of the result tensors is expected");
+  Py_ssize_t i = 0;
+  for (const auto& s : shapes) {
+    const at::Tensor& t = here(PyTuple_GET_ITEM(out, i++));
+    need(t.scalar_type() == at::kInt && t.sizes() == at::IntArrayRef(s) && t.is_contiguous(), "out: contiguous int32 tensors of the results' shapes are expected");
+    r.push_back(t);
+  }
+  return r;
+}
+PyObject* tuple_of(const std::vector<at::Tensor>& r) {
+  PyObject* t = PyTuple_New((Py_ssize_t)r.size());
+  if (!t) throw PyFailure();
+  for (size_t i = 0; i < r.size(); ++i) PyTuple_SET_ITEM(t, (Py_ssize_t)i, wrap(r[i]));
+  return t;
+}
+int32_t* ints_of(const at::Tensor& t) { return static_cast<int32_t*>(t.data_ptr()); }
+const at::Tensor& whole_table(PyObject* o) {
+  const at::Tensor& t = here(o);
+  need(t.scalar_type() == at::kInt && t.dim() == 2 && t.is_contiguous(), "the page table is int32 [sequences, pages], contiguous");
+  return t;
+}
+
+// (page_table, kv_len, source, add, n_pages, page_size, out or None) -> (page_table, kv_len, refs, copies, report)
+PyObject* pages_fork(PyObject* const* a) {
+  const at::Tensor& table = whole_table(a[0]);
+  const int64_t n = table.size(0), width = table.size(1), n_pages = integer(a[4]), page_size = integer(a[5]);
+  need(n_pages > 0 && n_pages <= INT32_MAX && page_size > 0 && page_size <= INT32_MAX, "n_pages and page_size must be positive");
+  const int32_t* len = ints(here(a[1]), n, "kv_len is int32 [sequences]");
+  const int32_t* source = ints(here(a[2]), n, "source is int32 [sequences]");
+  const int32_t* add = ints(here(a[3]), n, "add is int32 [sequences]");
+  const auto r = results(a[6], table, {{n, width}, {n}, {n_pages}, {n, 2}, {4}});
+  void* st = stream();
+  const int32_t* tp = ints_of(table);
+  int32_t* rp[5];
+  for (int i = 0; i < 5; ++i) rp[i] = ints_of(r[i]);
+  check(unlocked([&] {
+    return api.pages_fork((int32_t)n, (int32_t)width, (int32_t)n_pages, (int32_t)page_size, tp, len, source, add, rp[0], rp[1], rp[2], rp[3], rp[4], st);
+  }));
+  return tuple_of(r);
+}
+
+// (page_table, kv_len, n_pages, page_size, out or None) -> (page_table, refs, moves, report)
+PyObject* pages_compact(PyObject* const* a) {
+  const at::Tensor& table = whole_table(a[0]);
+  const int64_t n = table.size(0), width = table.size(1), n_pages = integer(a[2]), page_size = integer(a[3]);
+  need(n_pages > 0 && n_pages <= INT32_MAX && page_size > 0 && page_size <= INT32_MAX, "n_pages and page_size must be positive");
+  const int32_t* len = ints(here(a[1]), n, "kv_len is int32 [sequences]");
+  const auto r = results(a[4], table, {{n, width}, {n_pages}, {n_pages / 2, 2}, {4}});
+  void* st = stream();
+  const int32_t* tp = ints_of(table);
+  int32_t* rp[4];
+  for (int i = 0; i < 4; ++i) rp[i] = ints_of(r[i]);
+  check(unlocked([&] {
+    return api.pages_compact((int32_t)n, (int32_t)width, (int32_t)n_pages, (int32_t)page_size, tp, len, rp[0], rp[1], rp[2], rp[3], st);
+  }));
+  return tuple_of(r);
+}
+
+// (pools, pairs): pools = sequence of tensors [n_pages, ...] whose pages are dense
+PyObject* pages_copy(PyObject* const* a) {
+  constexpr Py_ssize_t kMost = 256;
+  void* at[kMost];
+  int64_t stride[kMost], bytes = 0, n_pages = 0;
+  const at::Tensor& pairs = here(a[1]);
+  need(pairs.scalar_type() == at::kInt && pairs.dim() == 2 && pairs.size(1) == 2 && pairs.is_contiguous(), "pairs is int32 [n, 2], contiguous");
+  need(PyList_Check(a[0]) || PyTuple_Check(a[0]), "pools: a list of tensors is expected");
+  const Py_ssize_t n = PySequence_Fast_GET_SIZE(a[0]);
+  if (n > kMost) raise_status(CASCADE_ERR_UNSUPPORTED, "cascade_pages_copy: more than 256 pools");
+  for (Py_ssize_t i = 0; i < n; ++i) {
+    const at::Tensor& t = here(PySequence_Fast_GET_ITEM(a[0], i));
+    need(t.dim() >= 2 && t.size(0) > 0, "a pool is [n_pages, ...]");
+    int64_t dense = 1;  // a page is dense if its strides are those of some order of its dimensions
+    bool used[8] = {};
+    need(t.dim() <= 8, "a pool has at most eight dimensions");
+    for (int64_t left = 1; left < t.dim(); ++left) {
+      int64_t next = -1;
+      for (int64_t j = 1; j < t.dim(); ++j)
+        if (!used[j] && (t.size(j) == 1 || t.stride(j) == dense)) {
+          next = j;
+          if (t.size(j) > 1) break;
+        }
+      need(next >= 0, "the pages of a pool must be dense");
+      used[next] = true;
+      dense *= t.size(next);
+    }
+    const int64_t es = (int64_t)t.element_size();
+    need(i == 0 || (dense * es == bytes && t.size(0) == n_pages), "all pools must have as many pages, of one size");
+    bytes = dense * es;
+    n_pages = t.size(0);
+    at[i] = t.data_ptr();
+    stride[i] = n_pages > 1 ? t.stride(0) * es : bytes;
+  }
+  need(n_pages <= INT32_MAX && pairs.size(0) <= INT32_MAX, "too many pages or pairs");
+  void* st = stream();
+  const int32_t* pp = ints_of(pairs);
+  const int32_t n_pairs = size(pairs, 0);
+  check(unlocked([&] { return api.pages_copy((int32_t)n, at, stride, bytes, (int32_t)n_pages, pp, n_pairs, st); }));
+  Py_RETURN_NONE;
+}
+
 // load(path of the CUDA library, CascadeError)
 PyObject* load(PyObject*, PyObject* args) {
   const char* path = nullptr;
@@ -342,6 +613,13 @@ PyObject* load(PyObject*, PyObject* args) {
   find(api.decode_step_rope, "cascade_decode_step_rope");
   find(api.decode_static, "cascade_attn_decode_static");
   find(api.plan_advance, "cascade_plan_advance");
+  find(api.rope_rows, "cascade_rope_rows");
+  find(api.paged_append, "cascade_paged_append");
+  find(api.attn_paged, "cascade_attn_paged");
+  find(api.attn_paged_workspace_bytes, "cascade_attn_paged_workspace_bytes");
+  find(api.pages_fork, "cascade_pages_fork");
+  find(api.pages_compact, "cascade_pages_compact");
+  find(api.pages_copy, "cascade_pages_copy");
   if (PyErr_Occurred()) return nullptr;
   Py_INCREF(error);
   Py_XDECREF(cascade_error);
@@ -362,6 +640,12 @@ PyMethodDef methods[] = {
     {"decode_step_rope", fast<12, decode_step_rope>(), METH_FASTCALL, nullptr},
     {"attn_decode_static", fast<7, attn_decode_static>(), METH_FASTCALL, nullptr},
     {"plan_advance", fast<2, plan_advance>(), METH_FASTCALL, nullptr},
+    {"rope_rows", fast<5, rope_rows>(), METH_FASTCALL, nullptr},
+    {"paged_append", fast<12, paged_append>(), METH_FASTCALL, nullptr},
+    {"attn_paged", fast<13, attn_paged>(), METH_FASTCALL, nullptr},
+    {"pages_fork", fast<7, pages_fork>(), METH_FASTCALL, nullptr},
+    {"pages_compact", fast<5, pages_compact>(), METH_FASTCALL, nullptr},
+    {"pages_copy", fast<2, pages_copy>(), METH_FASTCALL, nullptr},
     {nullptr, nullptr, 0, nullptr},
 };
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_fastcall", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};

@@ -1,0 +1,85 @@
+// What the kernels on paged caches share: the rows of a sequence, its length and its pages, each checked before it forms an
+// address, and the words that they report to.
+#pragma once
+
+#include "cascade_internal.cuh"
+
+namespace cascade {
+
+// Words 0 .. kStatusWords - 1: a bounded wait that gave up, as in a plan (WaitCtx).  Then a bad index: its code, the sequence (or
+// pair) and the value.
+enum PagedStatus { kBadIndexWord = 32, kPagedStatusWords = 36 };
+enum PagedBad {
+  kBadRowStart = 121,  // row_start falls, or leaves [0, n_rows]
+  kBadLength = 122,    // kv_len below 0, or more rows than the table has pages for
+  kBadPage = 123,      // a page id outside [0, n_pages)
+  kBadPosition = 124,  // a position outside the rotary table
+  kBadPair = 125,      // a page pair outside [0, n_pages)
+  kBadRows = 126       // a sequence has more rows than max_rows
+};
+
+__device__ __forceinline__ void paged_report(int32_t* status, int code, int where, int value) {
+  if (atomicCAS(status + kBadIndexWord, 0, code) == 0) {
+    status[kBadIndexWord + 1] = where;
+    status[kBadIndexWord + 2] = value;
+  }
+}
+
+// First row and number of rows of sequence b; none where row_start makes no sense.
+__device__ __forceinline__ int2 paged_rows(const PagedDev& g, int b) {
+  const int first = __ldg(g.row_start + b), end = __ldg(g.row_start + b + 1);
+  if (first < 0 || end < first || end > g.n_rows) {
+    paged_report(g.status, kBadRowStart, b, first);
+    return make_int2(0, 0);
+  }
+  return make_int2(first, end - first);
+}
+// Cache rows of sequence b, as many as its row of the table can hold.
+__device__ __forceinline__ int paged_len(const PagedDev& g, int b) {
+  const int len = __ldg(g.kv_len + b);
+  const int64_t most = (int64_t)g.max_pages * g.page_size;
+  if (len >= 0 && len <= most) return len;
+  paged_report(g.status, kBadLength, b, len);
+  return len < 0 ? 0 : (int)most;
+}
+// Id of page i of sequence b (i below max_pages); page 0 in the place of a bad one, which is reported.
+__device__ __forceinline__ int paged_page(const PagedDev& g, int b, int i) {
+  const int id = __ldg(g.table + (int64_t)b * g.table_stride + i);
+  if ((unsigned)id < (unsigned)g.n_pages) return id;
+  paged_report(g.status, kBadPage, b, id);
+  return 0;
+}
+// Cache rows that row i of the n of a sequence sees; `row` is its place among all rows.
+__device__ __forceinline__ int paged_seen(const PagedDev& g, bool causal, int n, int len, int i, int row) {
+  if (g.visible) return max(0, min(len, __ldg(g.visible + row)));
+  return causal ? max(0, len - n + i + 1) : len;
+}
+
+// Sequence and tile of tile number t, of those of `per_tile` rows each that the sequences of least .. most rows have, one sequence
+// after another; the last tile of a sequence (which sees most) comes first.  {sequence, tile}, or {-1, 0} past the last.  All lanes
+// of a warp.
+__device__ __forceinline__ int2 paged_tile(const PagedDev& g, int t, int per_tile, int lane) {
+  int before = 0;
+  for (int b0 = 0; b0 < g.batch; b0 += 32) {
+    const int b = b0 + lane;
+    const int n = b < g.batch ? paged_rows(g, b).y : 0;
+    const int tiles = n >= g.least && n <= g.most ? (n + per_tile - 1) / per_tile : 0;
+    int incl = tiles;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+      const int u = __shfl_up_sync(0xffffffffu, incl, o);
+      if (lane >= o) incl += u;
+    }
+    const int total = __shfl_sync(0xffffffffu, incl, 31);
+    if (t < before + total) {
+      const uint32_t past = __ballot_sync(0xffffffffu, before + incl > t);
+      const int who = __ffs(past) - 1;
+      const int end = before + __shfl_sync(0xffffffffu, incl, who);
+      return make_int2(b0 + who, end - 1 - t);
+    }
+    before += total;
+  }
+  return make_int2(-1, 0);
+}
+
+}  // namespace cascade
