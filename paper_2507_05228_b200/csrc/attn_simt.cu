@@ -654,6 +654,7 @@ cudaError_t launch_paged_alu(AttnParams p, cascade_dtype_t dtype, void* workspac
     p.m_part = static_cast<float*>(workspace) + items * p.d;
     p.l_part = p.m_part + items;
   }
+  TimedLaunch timed(stream);
   if (dtype == CASCADE_BF16) return p.d == 128 ? launch_paged<__nv_bfloat16, 128>(p, stream) : launch_paged<__nv_bfloat16, 64>(p, stream);
   return p.d == 128 ? launch_paged<float, 128>(p, stream) : launch_paged<float, 64>(p, stream);
 }

@@ -22,6 +22,10 @@
 // shards: at every shard boundary that shard's (u, m, l) is written out and the statistics and the accumulator start over.
 // (A CTA per (query tile, KV shard) pair would pay the CTA set-up once per pair.)
 //
+// Paged (kPaged, cascade_attn_paged).  As the fused route, with query tiles of 256 / Gp consecutive rows of one sequence of a ragged
+// batch, found from the row starts when the CTA runs, and with the keys of a tile in as many boxes as pages hold them: a loader's
+// lane looks up the page of one box each, a tile ahead.
+//
 // Warp roles (12 warps):
 //   0-3   softmax of sub-tile 0, 4-7 softmax of sub-tile 1: thread = MMA row = TMEM lane.  Reads the logits S with
 //         tcgen05.ld, applies the mask (the row sees a prefix of the keys), writes the weights P as bf16 back into the TMEM
@@ -51,9 +55,11 @@
 // Every mbarrier wait is bounded: on expiry the CTA raises a flag, records a code in the plan's status word
 // and drains without waiting again.
 #include <float.h>
+#include <limits.h>
 
 #include <algorithm>
 
+#include "paged.cuh"
 #include "tcgen05.cuh"
 
 namespace cascade {
@@ -126,11 +132,12 @@ enum Bar {
   P_FULL = S_FULL + 4,              // [2]; kRing: [2][2], see p_full
   O_FULL = P_FULL + 4,              // [2] the last product of a sub-tile is in
   CHECKED = O_FULL + 2,             // [1] the plan's status word has been looked at
-  O_RDY = CHECKED + 1               // [2]  kWalk: the accumulator of a sub-tile holds a finished shard;
+  O_RDY = CHECKED + 1,              // [2]  kWalk: the accumulator of a sub-tile holds a finished shard;
                                     //      kRing: the product of a sub-tile's latest tile is in its accumulator
+  V_TAIL = O_RDY + 2                // [1]  kPaged: the V tile in which the sequence ends has arrived
 };
 constexpr int kBars = O_RDY + 2;
-static_assert(kBars <= Cfg<128, false>::kNumBars && kBars <= 32, "barrier table too small");
+static_assert(kBars < Cfg<128, false>::kNumBars && kBars < 32, "barrier table too small");
 
 // TMA box loads, 64 elements wide: rows land as 128 bytes each.  32 rows of the 3-D tensor [matrix z][row y][column x]
 // (shard-major copies), or 128 rows of the 4-D tensor [sequence w][head z][row y][column x].
@@ -232,6 +239,9 @@ struct TmaArgs {
   // tokens x Gp heads, 64 columns
   int q_valid;  // 0: the threads load them
   CUtensorMap q;
+  // kPaged: k and v are [pages][kv_heads][rows of a page][head_dim], a box 1 << box_log2 rows of a page; q is [1][rows of all
+  // sequences][heads][head_dim]
+  int box_log2;
 };
 
 // kRope: the query rows are turned by the rotary embedding of their positions while they are staged (the key rows
@@ -240,7 +250,7 @@ struct TmaArgs {
 // one after another): the shards are walked as in the fused mode, but a tile never mixes two shards, and at a shard
 // boundary the softmax threads write that shard's (u, m, l) out and start over.  The query tile, the TMEM allocation,
 // the barriers and the K/V pipelines are set up once per query tile instead of once per (query tile, KV shard).
-template <int D, bool kRope, bool kWalk, bool kBoxes>
+template <int D, bool kRope, bool kWalk, bool kBoxes, bool kPaged>
 __global__ void __launch_bounds__(kThreads, 1) attn_tc_kernel(const __grid_constant__ AttnParams p, int lg,
                                                               int tile_major, int lg_split, int early, int after_gather,
                                                               const __grid_constant__ TmaArgs tma) {
@@ -293,7 +303,7 @@ __global__ void __launch_bounds__(kThreads, 1) attn_tc_kernel(const __grid_const
   // for it.
   grid_go();
   if (!after_gather) grid_wait();
-  const int map = pl.n_maps == 1 ? 0 : b;
+  const int map = kPaged || pl.n_maps == 1 ? 0 : b;
   const int h0 = hg * Gp;  // first of the Gp stacked heads
   const int per_kv = p.G >> lg;  // head groups per KV head
   const int g = per_kv == 1 ? hg : hg / per_kv;
@@ -306,9 +316,21 @@ __global__ void __launch_bounds__(kThreads, 1) attn_tc_kernel(const __grid_const
       grid_wait();
       return;
     }
-  } else {
+  } else if constexpr (!kPaged) {
     row0 = (n_qt - 1 - tile_idx) * 2 * R;
     nrows = min(2 * R, pl.n_q - row0);
+  }
+  int seq_row0 = 0, seq_rows = 0, seq_len = 0;  // kPaged: first row, number of rows and cache rows of the sequence; row0 is from its first
+  if constexpr (kPaged) {
+    const int2 t = paged_tile(p.paged, tile_idx, 2 * R, (int)threadIdx.x & 31);
+    if (t.x < 0) return;  // (uniform for the cluster: fewer tiles than there might have been)
+    b = t.x;
+    const int2 rows = paged_rows(p.paged, b);
+    seq_row0 = rows.x;
+    seq_rows = rows.y;
+    seq_len = paged_len(p.paged, b);
+    row0 = t.y * 2 * R;
+    nrows = min(2 * R, seq_rows - row0);
   }
   const int n_sub = nrows > R ? 2 : 1;
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
@@ -318,14 +340,25 @@ __global__ void __launch_bounds__(kThreads, 1) attn_tc_kernel(const __grid_const
   // Token of a row, and (not kWalk) how many K/V rows it sees: a prefix of the tensors, because the mask is causal in
   // positions and the rows ascend in position.
   auto token_of = [&](int row) {
-    return kWalk ? (int)CASCADE_CHECKED((int64_t)__ldg(q_idx + row), pl.n_q, pl.status, 108) : row;
+    return kWalk ? (int)CASCADE_CHECKED((int64_t)__ldg(q_idx + row), pl.n_q, pl.status, 108) : kPaged ? seq_row0 + row : row;
   };
   auto seen_by = [&](int token) {
+    if constexpr (kPaged) return paged_seen(p.paged, pl.causal, seq_rows, seq_len, token, seq_row0 + token);
     if (!pl.causal) return pl.n_kv;
     if (!p.prefix_from_vis) return (int)max((int64_t)0, min((int64_t)pl.n_kv, (int64_t)pl.q_pos_offset + token + 1));
     const int32_t* v = vis + (size_t)__ldg(pl.q_inv + (size_t)map * pl.n_q + token) * P;  // rows at positions of their own
     int n = 0;
     for (int kk = 0; kk < P; ++kk) n += __ldg(v + kk);
+    return n;
+  };
+  auto most_seen = [&]() {  // by any row of the CTA (all lanes of a warp; given prefixes may come in any order)
+    int n = seen_by(row0 + nrows - 1);
+    if constexpr (kPaged) {
+      if (p.paged.visible) {
+        for (int r = (int)threadIdx.x & 31; r < nrows; r += 32) n = max(n, seen_by(row0 + r));
+        n = __reduce_max_sync(0xffffffffu, n);
+      }
+    }
     return n;
   };
   // Query sub-tiles (row r = slot r / Gp, head r % Gp): the 128 softmax threads of a sub-tile gather it from the
@@ -340,6 +373,7 @@ __global__ void __launch_bounds__(kThreads, 1) attn_tc_kernel(const __grid_const
   const float4* rope_row[kRope ? 8 : 1];  // this thread's slice of the table row of each of its query rows
   float4 cs[kRope ? 4 : 1][4];            // (cos, sin) of four rows: 8 pairs each
   const bool q_boxes = !kWalk && !kRope && tma.q_valid;
+  const int64_t b_rows = kPaged ? 0 : b;  // which sequence's tensor the rows are of
   if (!q_boxes && warp < 8 && (warp >> 2) < n_sub) {
     const int s = warp >> 2;
     const int sub_row0 = row0 + s * R;
@@ -348,7 +382,7 @@ __global__ void __launch_bounds__(kThreads, 1) attn_tc_kernel(const __grid_const
       // Rotary staging: a thread holds both halves of 8 rotation pairs of a row (columns 8 c .. and 64 + 8 c ..),
       // 8 threads per row, 8 rows per thread, and the (cos, sin) of the first four of its rows; the table rows of the
       // other four are fetched while those are turned.
-      const __nv_bfloat16* qb = static_cast<const __nv_bfloat16*>(p.q) + (int64_t)b * p.qs.batch + (tid & 7) * 8;
+      const __nv_bfloat16* qb = static_cast<const __nv_bfloat16*>(p.q) + b_rows * p.qs.batch + (tid & 7) * 8;
 #pragma unroll
       for (int j = 0; j < 8; ++j) {
         const int r = (tid >> 3 & 15) + 16 * j;
@@ -364,7 +398,7 @@ __global__ void __launch_bounds__(kThreads, 1) attn_tc_kernel(const __grid_const
 #pragma unroll
         for (int e = 0; e < 4; ++e) cs[j][e] = __ldg(rope_row[j] + e);
     } else {
-      const __nv_bfloat16* qb = static_cast<const __nv_bfloat16*>(p.q) + (int64_t)b * p.qs.batch + q_chunk * 8;
+      const __nv_bfloat16* qb = static_cast<const __nv_bfloat16*>(p.q) + b_rows * p.qs.batch + q_chunk * 8;
 #pragma unroll
       for (int j = 0; j < kRowChunks; ++j) {
         const int r = q_row + kRowsPerPass * j;
@@ -405,7 +439,19 @@ __global__ void __launch_bounds__(kThreads, 1) attn_tc_kernel(const __grid_const
       }
     } else {
       // the keys the last row sees, in tiles of 128 from the first on; this CTA takes its part of the tiles
-      const int seen = lane < 3 ? seen_by(lane == 0 ? row0 + nrows - 1 : row0 + (lane == 2 ? (n_sub - 1) * R : 0)) : 0;
+      int seen = lane < 3 ? seen_by(lane == 0 ? row0 + nrows - 1 : row0 + (lane == 2 ? (n_sub - 1) * R : 0)) : 0;
+      if constexpr (kPaged) {
+        if (p.paged.visible) {  // lane 0: the longest prefix, lanes 1 and 2: the shortest of each sub-tile
+          const int most = most_seen();
+          for (int s = 0; s < n_sub; ++s) {
+            int least = INT_MAX;
+            for (int r = s * R + lane; r < min(nrows, (s + 1) * R); r += 32) least = min(least, seen_by(row0 + r));
+            least = __reduce_min_sync(0xffffffffu, least);
+            if (lane == 1 + s) seen = least;
+          }
+          if (lane == 0) seen = most;
+        }
+      }
       const int tiles = (__shfl_sync(0xffffffffu, seen, 0) + kNMax - 1) / kNMax;
       const int t0 = tiles * part_of_keys >> lg_split, t1 = tiles * (part_of_keys + 1) >> lg_split;
       if (lane == 0) {
@@ -429,7 +475,7 @@ __global__ void __launch_bounds__(kThreads, 1) attn_tc_kernel(const __grid_const
   // Warp 9 sets the barriers up, a lane each, and has the first data on their way.  (A barrier that nobody else waits for it at, past
   // the requests, costs the softmax threads registers: partials of 4099 tokens in 16 shards 392 -> 418 us.)
   if (warp == 9) {
-    if (lane < kBars) {  // one arrival, except by the threads of a sub-tile; TMA: one that announces the byte count, then the bytes
+    if (lane < kBars + (kPaged ? 1 : 0)) {  // one arrival, except by the threads of a sub-tile; TMA: one that announces the byte count, then the bytes
       const bool by_rows = lane < Q_FULL + 2 ? !q_boxes : lane >= P_FULL && lane < P_FULL + 4;
       mbar_init(bar(lane), by_rows ? 128u : 1u);
     }
@@ -438,19 +484,20 @@ __global__ void __launch_bounds__(kThreads, 1) attn_tc_kernel(const __grid_const
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     __syncwarp();
     if constexpr (!kWalk) {
+      const int cta_sees = kPaged ? most_seen() : 0;
       if (lane == 0) {
         // The query rows and the first tiles of K and V (early, bit 0: K, bit 1: V; not what a gather in front of this grid
         // writes) are requested here, under the rest of the set-up.  (Query rows loaded by the softmax threads cost a CTA 2700
         // cycles before its first product: 2048 tokens 40.3 -> 38.5 us, 2 x 3001 tokens of head_dim 64 78.2 -> 76.7.)
-        const int tiles = (seen_by(row0 + nrows - 1) + kNMax - 1) / kNMax;
+        const int tiles = ((kPaged ? cta_sees : seen_by(row0 + nrows - 1)) + kNMax - 1) / kNMax;
         const int t0 = tiles * part_of_keys >> lg_split;
         if (tiles * (part_of_keys + 1) >> lg_split > t0) {
           asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
           auto request_q = [&](int s) {
             mbar_expect_tx(bar(Q_FULL + s), (uint32_t)kTileBytes);
             for (int half = 0; half < C::kHalves; ++half)
-              tma_tile4(smem_base + (uint32_t)(kOffQ + s * kTileBytes + half * kHalfBytes), &tma.q, 64 * half, h0, row0 + s * R, b,
-                        bar(Q_FULL + s));
+              tma_tile4(smem_base + (uint32_t)(kOffQ + s * kTileBytes + half * kHalfBytes), &tma.q, 64 * half, h0,
+                        seq_row0 + row0 + s * R, (int)b_rows, bar(Q_FULL + s));
           };
           auto request_kv = [&](const CUtensorMap* map, uint32_t dst, uint32_t fb) {
             mbar_expect_tx(fb, (uint32_t)kTileBytes);
@@ -949,7 +996,7 @@ __global__ void __launch_bounds__(kThreads, 1) attn_tc_kernel(const __grid_const
           }
         }
         const float inv = l_all > 0.f ? 1.f / (l_all + fix_all) : 0.f;
-        __nv_bfloat16* dst = static_cast<__nv_bfloat16*>(p.o_out) + (int64_t)b * p.os.batch + (int64_t)slot * p.os.token +
+        __nv_bfloat16* dst = static_cast<__nv_bfloat16*>(p.o_out) + b_rows * p.os.batch + (int64_t)(seq_row0 + slot) * p.os.token +
                              (int64_t)head * p.os.head + me * cols;
         for (int c0 = 0; c0 < cols; c0 += 8) {
           float acc[8];
@@ -981,7 +1028,7 @@ __global__ void __launch_bounds__(kThreads, 1) attn_tc_kernel(const __grid_const
           }
         }
         if (out_ok && me == 0 && p.lse_out)
-          p.lse_out[((int64_t)b * pl.n_q + slot) * p.H + head] =
+          p.lse_out[(b_rows * pl.n_q + seq_row0 + slot) * p.H + head] =
               l_all > 0.f ? (m_use + log2f(l_all)) * 0.6931471805599453f : -INFINITY;
       } else {
       // ---- epilogue
@@ -990,8 +1037,8 @@ __global__ void __launch_bounds__(kThreads, 1) attn_tc_kernel(const __grid_const
       int64_t stat = 0;
       if (row_ok) {
         if (!kWalk && p.fused) {
-          stat = ((int64_t)b * pl.n_q + slot) * p.H + head;
-          dst = static_cast<__nv_bfloat16*>(p.o_out) + (int64_t)b * p.os.batch + (int64_t)slot * p.os.token +
+          stat = (b_rows * pl.n_q + seq_row0 + slot) * p.H + head;
+          dst = static_cast<__nv_bfloat16*>(p.o_out) + b_rows * p.os.batch + (int64_t)(seq_row0 + slot) * p.os.token +
                 (int64_t)head * p.os.head;
         } else {
           // kWalk: the last shard the CTA saw anything of; its other shards were written on the way.  Otherwise there is
@@ -1268,7 +1315,18 @@ __global__ void __launch_bounds__(kThreads, 1) attn_tc_kernel(const __grid_const
         // (a no-op otherwise).  Nothing else in this kernel reads what the gather grid writes.
         grid_wait();
         int n_issued = 0;
+        // kPaged: where a box of this lane's comes from in tile i: row of the page and page; past the sequence's last row, where
+        // the table has no page, a page that does not exist, which reads as zeros
+        auto box_of = [&](int i) {
+          const int key = key0 + kNMax * i + (lane << tma.box_log2), index = key / p.paged.page_size;
+          const bool there = i < n_tiles && lane << tma.box_log2 < kNMax && key < seq_len;
+          return make_int2(key - index * p.paged.page_size, there ? paged_page(p.paged, b, index) : p.paged.n_pages);
+        };
+        int2 box = make_int2(0, 0);
+        if constexpr (kPaged) box = box_of(0);
         for (int i = 0; i < n_tiles; ++i) {
+          int2 box_next = make_int2(0, 0);
+          if constexpr (kPaged) box_next = box_of(i + 1);
           const int nch = kWalk ? min(4, cur.nc - cur.c) : tile_chunks(i);
           const int st = i % n_stages;
           note(8 * i + 1);
@@ -1276,7 +1334,37 @@ __global__ void __launch_bounds__(kThreads, 1) attn_tc_kernel(const __grid_const
           // requested early before this warp gets here, and a wait for the phase before that would never end.
           if (i >= n_stages && !wait_bar(wc, bar(empty0 + st), (uint32_t)(((i / n_stages) & 1) ^ 1), is_k ? 9 : 10, i)) break;
           const uint32_t dst = tiles_s + (uint32_t)(st * kTileBytes), fb = bar(full0 + st);
-          if constexpr (kWalk) {
+          if constexpr (kPaged) {
+            // The page in which the sequence ends holds anything behind its last row.  A key there is masked, but a weight of 0
+            // times NaN is NaN: the values are overwritten with zeros before the tile counts as full.
+            const int end = seq_len - (key0 + kNMax * i), box_rows = 1 << tma.box_log2;
+            const bool tail = !is_k && end < kNMax && (end & (box_rows - 1)) != 0;
+            const uint32_t arrives = tail ? bar(V_TAIL) : fb;
+            if (leader) mbar_expect_tx(arrives, (uint32_t)kTileBytes);
+            __syncwarp();
+            if (lane << tma.box_log2 < kNMax) {
+              const uint32_t to = dst + (uint32_t)((lane << tma.box_log2) * 128);
+              tma_tile4(to, map, 0, box.x, g, box.y, arrives);
+              if (C::kHalves == 2) tma_tile4(to + (uint32_t)kHalfBytes, map, 64, box.x, g, box.y, arrives);
+            }
+            if (tail) {
+              const bool here = wait_bar(wc, arrives, 0u, 12, i);
+              if (!here) {
+                landed(arrives, 0u);
+                break;
+              }
+              const int rows = box_rows - (end & (box_rows - 1));
+              for (int e = lane; e < rows * 8 * C::kHalves; e += 32) {
+                const int half = e / (rows * 8), at = e - half * rows * 8;
+                asm volatile("st.shared.v4.b32 [%0], {%1, %1, %1, %1};" ::"r"(dst + (uint32_t)(half * kHalfBytes + end * 128 + at * 16)), "r"(0)
+                             : "memory");
+              }
+              asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+              __syncwarp();
+              if (leader) mbar_arrive(fb);
+            }
+            box = box_next;
+          } else if constexpr (kWalk) {
             if (leader) mbar_expect_tx(fb, (uint32_t)(nch * C::kHalves * kChunkBytes));
             for (int ch = 0; ch < nch; ++ch) {
               // A chunk is 32 consecutive rows of the shard-major copy.  Rows past the shard's visible prefix belong
@@ -1397,20 +1485,22 @@ struct TcLaunch {
   int lg, tile_major, lg_split, early;
   bool after_gather;
   bool boxes;  // partials at head_dim 128
+  bool paged;
 };
 
 cudaError_t launch_kernel(const AttnParams& p, bool walk, const TcLaunch& l, int64_t n_tiles, const tc::TmaArgs& tma,
                           cudaStream_t stream) {
-  auto kernel = p.d == 64 ? (walk ? tc::attn_tc_kernel<64, false, true, true> : tc::attn_tc_kernel<64, false, false, false>)
-                : p.rope  ? tc::attn_tc_kernel<128, true, false, false>
-                : !walk   ? tc::attn_tc_kernel<128, false, false, false>
-                          : (l.boxes ? tc::attn_tc_kernel<128, false, true, true> : tc::attn_tc_kernel<128, false, true, false>);
+  auto kernel = l.paged   ? (p.d == 64 ? tc::attn_tc_kernel<64, false, false, false, true> : tc::attn_tc_kernel<128, false, false, false, true>)
+                : p.d == 64 ? (walk ? tc::attn_tc_kernel<64, false, true, true, false> : tc::attn_tc_kernel<64, false, false, false, false>)
+                : p.rope  ? tc::attn_tc_kernel<128, true, false, false, false>
+                : !walk   ? tc::attn_tc_kernel<128, false, false, false, false>
+                          : (l.boxes ? tc::attn_tc_kernel<128, false, true, true, false> : tc::attn_tc_kernel<128, false, true, false, false>);
   const int smem_bytes = p.d == 64 ? (walk ? tc::Cfg<64, true>::kSmemBytes : tc::Cfg<64, false>::kSmemBytes)
                                    : (l.boxes ? tc::Cfg<128, true>::kSmemBytes : tc::Cfg<128, false>::kSmemBytes);
   cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem_bytes);
   if (e != cudaSuccess) return e;
   // (few CTAs if tile_major; a head group has a head, so n_hg and the batch fit the short axes as the entry points check)
-  const unsigned n_hg = (unsigned)(p.H >> l.lg), batch = (unsigned)p.batch, tiles = (unsigned)n_tiles;
+  const unsigned n_hg = (unsigned)(p.H >> l.lg), batch = l.paged ? 1u : (unsigned)p.batch, tiles = (unsigned)n_tiles;
   const dim3 grid = l.tile_major ? dim3(n_hg << l.lg_split, batch, tiles) : dim3(tiles, n_hg, batch);
   TimedLaunch timed(stream);
   return launch_dependent(kernel, grid, tc::kThreads, smem_bytes, 1u << l.lg_split, !walk || l.after_gather, stream, p, l.lg,
@@ -1466,7 +1556,7 @@ cudaError_t launch_attn_tc_partials(const AttnParams& p, const void* k_sorted, c
                                     {n_q * p.H * p.d, (int64_t)p.H * p.d, p.d});
   const int64_t n_ctas = n_tiles * (p.H >> lg) * p.batch;
   // few CTAs per SM: balance matters more than L2 locality
-  const TcLaunch l = {lg, n_ctas <= 8 * (int64_t)sm_count(), 0, 0, true, boxes && tma.o_valid};
+  const TcLaunch l = {lg, n_ctas <= 8 * (int64_t)sm_count(), 0, 0, true, boxes && tma.o_valid, false};
   return launch_kernel(p, true, l, n_tiles, tma, stream);
 }
 
@@ -1496,8 +1586,51 @@ cudaError_t launch_attn_tc(const AttnParams& p, const TcRows& k, const TcRows& v
       if (rule_ctas << i <= fit[i] && key_tiles >= (p.d == 64 ? 2 : 3) << i) lg_split = i;
   }
   const TcLaunch l = {lg, n_ctas <= 8 * (int64_t)sm_count(), lg_split,
-                      p.prefix_from_vis ? 0 : (k_gathered ? 0 : 1) | (v_gathered ? 0 : 2), k_gathered || v_gathered, false};
+                      p.prefix_from_vis ? 0 : (k_gathered ? 0 : 1) | (v_gathered ? 0 : 2), k_gathered || v_gathered, false, false};
   return launch_kernel(p, false, l, n_qt, tma, stream);
+}
+
+// K or V pages as [page][kv_head][row of the page][d]; box = rows of a page that a tile of 128 keys takes at a time, 64 columns.
+static bool encode_pages(CUtensorMap* map, const void* base, const Strides& st, const AttnParams& p, int box_log2) {
+  EncodeTiledFn fn = encode_tiled_fn();
+  if (!fn) return false;
+  const PagedDev& g = p.paged;
+  const cuuint64_t dims[4] = {(cuuint64_t)p.d, (cuuint64_t)g.page_size, (cuuint64_t)p.Hkv, (cuuint64_t)g.n_pages};
+  auto stride = [&](int64_t elems, int64_t extent) { return (cuuint64_t)(extent > 1 ? elems * 2 : p.d * 2); };
+  const cuuint64_t strides[3] = {stride(st.token, g.page_size), stride(st.head, p.Hkv), stride(st.batch, g.n_pages)};
+  const cuuint32_t box[4] = {64, 1u << box_log2, 1, 1};
+  const cuuint32_t estr[4] = {1, 1, 1, 1};
+  return fn(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 4, const_cast<void*>(base), dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
+            CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+bool paged_tc_takes(const AttnParams& p) {
+  return tc_rows_loadable({p.k, p.ks}, p.paged.page_size, p.Hkv, p.paged.n_pages) &&
+         tc_rows_loadable({p.v, p.vs}, p.paged.page_size, p.Hkv, p.paged.n_pages);
+}
+
+cudaError_t launch_paged_tc(const AttnParams& p, cudaStream_t stream) {
+  const PagedDev& g = p.paged;
+  tc::TmaArgs tma = {};
+  while (tma.box_log2 < 7 && g.page_size % (2 << tma.box_log2) == 0) ++tma.box_log2;
+  if (!encode_pages(&tma.k, p.k, p.ks, p, tma.box_log2) || !encode_pages(&tma.v, p.v, p.vs, p, tma.box_log2)) {
+    set_error("cascade_attn_paged: could not build the TMA descriptors of the pages");
+    return cudaErrorInvalidValue;
+  }
+  const int lg = stacked_log2(p.G);
+  AttnParams rows = p;  // the rows of all sequences as one
+  rows.batch = 1;
+  rows.plan.n_q = g.n_rows;
+  tma.q_valid = encode_queries(&tma.q, rows, lg);
+  // Every sequence can end in a tile that is not full.  The rules below go by the tiles there are if the rows are one sequence's.
+  const int64_t per = 256 >> lg, least = (g.n_rows + per - 1) / per, bound = g.batch == 1 ? least : std::min<int64_t>(g.n_rows, g.n_rows / per + g.batch);
+  const int64_t heads = p.H >> lg, key_tiles = ((int64_t)g.max_pages * g.page_size + 127) / 128;
+  int lg_split = 0;  // as launch_attn_tc, by the keys that the table can hold
+  const int64_t fit[4] = {148, 148, 132, 120};
+  for (int i = 1; i < 4; ++i)
+    if ((least * heads) << i <= fit[i] && key_tiles >= (p.d == 64 ? 2 : 3) << i) lg_split = i;
+  const TcLaunch l = {lg, bound * heads <= 8 * (int64_t)sm_count(), lg_split, 0, false, false, true};
+  return launch_kernel(p, false, l, bound, tma, stream);
 }
 
 }  // namespace cascade

@@ -297,6 +297,9 @@ int32_t* paged_status_words();
 int paged_alu_parts(const AttnParams& p);
 size_t paged_alu_ws_bytes(const AttnParams& p);
 cudaError_t launch_paged_alu(AttnParams p, cascade_dtype_t dtype, void* workspace, cudaStream_t stream);
+// bf16 on the tensor cores, where a tensor map holds the pages
+bool paged_tc_takes(const AttnParams& p);
+cudaError_t launch_paged_tc(const AttnParams& p, cudaStream_t stream);
 
 // Rows turned by their positions and, with pages, appended (cascade_rope_rows, cascade_paged_append)
 struct RopeRowsParams {

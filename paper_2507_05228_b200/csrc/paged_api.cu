@@ -337,14 +337,14 @@ cascade_status_t cascade_attn_paged(cascade_dtype_t dtype, int32_t batch, int32_
   p.q = q;
   p.k = k_pages;
   p.v = v_pages;
-  p.qs = in(q_strides);
+  p.qs = {0, q_strides.token, q_strides.head};
   p.ks = in(k_page_strides);
   p.vs = in(v_page_strides);
   p.scale = scale;
   p.o_out = o_out;
-  p.os = in(o_strides);
+  p.os = {0, o_strides.token, o_strides.head};
   p.lse_out = lse_out;
-  TimedLaunch timed((cudaStream_t)stream);
+  if (dtype == CASCADE_BF16 && paged_tc_takes(p)) return launched(launch_paged_tc(p, (cudaStream_t)stream), fn);
   return launched(launch_paged_alu(p, dtype, workspace, (cudaStream_t)stream), fn);
 }
 
