@@ -22,45 +22,9 @@
 #include <atomic>
 #include <type_traits>
 
-#include "cascade_internal.cuh"
+#include "decode_common.cuh"
 
 namespace cascade {
-
-__device__ __forceinline__ float ex2f(float x) {
-  float y;
-  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
-  return y;
-}
-
-__device__ __forceinline__ void mma_16816(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3,
-                                          uint32_t b0, uint32_t b1) {
-  asm volatile(
-      "mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
-      : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
-      : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
-}
-
-// 8 x 8 transpose of 16-bit elements across a warp (lane (x, j) holds row x, columns 2j and 2j + 1)
-__device__ __forceinline__ uint32_t transpose8(uint32_t v) {
-  uint32_t r;
-  asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(r) : "r"(v));
-  return r;
-}
-
-__device__ __forceinline__ uint32_t pack2_bf16(float lo, float hi) {
-  const __nv_bfloat162 h = __floats2bfloat162_rn(lo, hi);
-  return *reinterpret_cast<const uint32_t*>(&h);
-}
-
-// 32 bytes, streaming; volatile so that the loads stay where the pipeline below puts them
-__device__ __forceinline__ void load32(const __nv_bfloat16* p, uint32_t* r) {
-#pragma unroll
-  for (int i = 0; i < 8; i += 4)
-    asm volatile("ld.global.cs.v4.b32 {%0, %1, %2, %3}, [%4];"
-                 : "=r"(r[i]), "=r"(r[i + 1]), "=r"(r[i + 2]), "=r"(r[i + 3])
-                 : "l"(p + 2 * i)
-                 : "memory");
-}
 
 // Query fragments of a CTA in shared memory: B operand of k-step s, lane (x = head, j) -> its two registers.
 struct DecodeQuery {

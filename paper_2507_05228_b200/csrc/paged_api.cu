@@ -277,9 +277,22 @@ AttnParams paged_shape(int32_t batch, int32_t n_rows, int32_t max_rows, int32_t 
   p.paged.most = max_rows;
   return p;
 }
-size_t paged_ws_bytes(const AttnParams& p, cascade_dtype_t dtype) {
-  (void)dtype;
-  return paged_alu_ws_bytes(p);
+// Which kernels take the sequences of a bf16 call: those of at most `rows` rows the decode kernel (0: none), the others the tensor-core
+// kernel on tiles.  (The ALU kernel takes all where no tensor map holds the pages.)
+struct PagedRoute {
+  int rows;
+  bool tiles;
+};
+PagedRoute paged_route(const AttnParams& p, int32_t max_rows) {
+  const int few = paged_decode_rows(p);
+  if (std::min(max_rows, p.paged.n_rows) <= few) return {std::min(max_rows, p.paged.n_rows), false};
+  return {p.paged.batch == 1 ? 0 : few, true};  // (one sequence: its rows are max_rows, unless they are padded)
+}
+size_t align256(size_t n) { return (n + 255) / 256 * 256; }
+size_t paged_ws_bytes(const AttnParams& p, cascade_dtype_t dtype, int32_t max_rows) {
+  if (dtype == CASCADE_F32) return paged_alu_ws_bytes(p);
+  const PagedRoute r = paged_route(p, max_rows);
+  return std::max(r.rows > 0 ? align256(paged_decode_ws_bytes(p, r.rows)) : 0, r.tiles ? paged_alu_ws_bytes(p) : 0);
 }
 
 }  // namespace
@@ -298,7 +311,7 @@ cascade_status_t cascade_attn_paged_workspace_bytes(cascade_dtype_t dtype, int32
     return fail(CASCADE_ERR_INVALID_ARG, fn, "sizes must be positive");
   s = check_sizes(fn, n_heads, n_kv_heads, page_size, max_pages);
   if (s != CASCADE_OK) return s;
-  *out_bytes = paged_ws_bytes(paged_shape(batch, n_rows, max_rows, n_heads, n_kv_heads, head_dim, page_size, max_pages), dtype);
+  *out_bytes = paged_ws_bytes(paged_shape(batch, n_rows, max_rows, n_heads, n_kv_heads, head_dim, page_size, max_pages), dtype, max_rows);
   return CASCADE_OK;
 }
 
@@ -325,7 +338,7 @@ cascade_status_t cascade_attn_paged(cascade_dtype_t dtype, int32_t batch, int32_
       !aligned4(lse_out))
     return fail(CASCADE_ERR_INVALID_ARG, fn, "pointers and row strides must be 16-byte aligned");
   AttnParams p = paged_shape(batch, n_rows, max_rows, n_heads, n_kv_heads, head_dim, page_size, max_pages);
-  const size_t need = paged_ws_bytes(p, dtype);
+  const size_t need = paged_ws_bytes(p, dtype, max_rows);
   if (need > 0 && (!workspace || workspace_bytes < need || ((uintptr_t)workspace & 255))) {
     set_error("%s: workspace of %zu bytes (256-byte aligned) required, got %zu", fn, need, workspace ? workspace_bytes : (size_t)0);
     return CASCADE_ERR_WORKSPACE;
@@ -344,8 +357,22 @@ cascade_status_t cascade_attn_paged(cascade_dtype_t dtype, int32_t batch, int32_
   p.o_out = o_out;
   p.os = {0, o_strides.token, o_strides.head};
   p.lse_out = lse_out;
-  if (dtype == CASCADE_BF16 && paged_tc_takes(p)) return launched(launch_paged_tc(p, (cudaStream_t)stream), fn);
-  return launched(launch_paged_alu(p, dtype, workspace, (cudaStream_t)stream), fn);
+  cudaStream_t st = (cudaStream_t)stream;
+  if (dtype == CASCADE_F32) return launched(launch_paged_alu(p, dtype, workspace, st), fn);
+  const PagedRoute r = paged_route(p, max_rows);
+  if (r.tiles && !paged_tc_takes(p)) return launched(launch_paged_alu(p, dtype, workspace, st), fn);
+  cudaError_t e = cudaSuccess;
+  if (r.rows > 0) {
+    AttnParams few = p;
+    few.paged.most = r.rows;
+    few.alone = !r.tiles;
+    e = launch_paged_decode(few, r.rows, workspace, st);
+  }
+  if (e == cudaSuccess && r.tiles) {
+    p.paged.least = r.rows + 1;
+    e = launch_paged_tc(p, st);
+  }
+  return launched(e, fn);
 }
 
 static cascade_status_t check_tables(const char* fn, int32_t n_seqs, int32_t width, int32_t n_pages, int32_t page_size, const void* a,

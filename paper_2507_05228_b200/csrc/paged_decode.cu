@@ -1,0 +1,581 @@
+// Single tokens and drafts over a paged cache (cascade_attn_paged for sequences of few rows), bf16: every K/V row is read once, so
+// the bound is HBM for large batches and latency for small ones.
+//
+// The columns of warp-level mma.m16n8k16 products are (row, head) pairs: the rows of a sequence times the heads of a KV head (as many
+// as divide its group, 16 at most), 8 or 16 of them.  A warp walks blocks of 16 keys, which lie in one page, with the fragments
+// straight from global memory, as decode.cu does and says why.  The weights go into the second product as two bf16 parts, the upper
+// 16 bits and the rest, so that they keep 16 bits of mantissa: the loads are the limit, and with one part the rounding of few rows
+// of weights was most of the error (2500 rows, 32 heads: 2.4e-3 of the output, 1.7e-3 with two, which is its own rounding).
+//
+// How the keys are shared out.
+//   Few (sequence, KV head) items: a cluster of CTAs has one and adds up in distributed shared memory; one launch.
+//   Many: lengths differ between sequences, so the 16-key blocks of all items, one after another, are cut into as many equal ranges as
+//   CTAs are resident; an item that a range covers whole is finished there, one that is cut leaves partials, which a second, small
+//   kernel adds up (a CTA for each place where an item is first cut).  Where the ranges start follows from the lengths, which only
+//   the device knows: every CTA adds the blocks up for itself.
+#include <algorithm>
+#include <type_traits>
+
+#include "decode_common.cuh"
+#include "paged.cuh"
+
+namespace cascade {
+
+namespace {
+
+constexpr int kWarps = 8, kThreads = kWarps * 32;
+constexpr int kMaxGroups = 2048;  // groups of 32 sequences
+constexpr int kClusterMost = 16;
+
+// Where a CTA's range starts: the item that holds its first block, and that block's place in the item.
+struct RangeStart {
+  int32_t b, item, before, blocks;  // blocks: of the item
+  int64_t total;                    // of all items
+};
+
+struct DecodeArgs {
+  int32_t Gi, items;  // heads of an item, items of a sequence
+  int32_t n_cta;      // CTAs of the grid (ranges), or of a cluster
+  RangeStart* starts;  // [n_cta]
+  float* partials;     // [n_cta][2][columns][D + 2]: of an item that starts before the range, and of one that ends behind it
+};
+
+// 16-key blocks of sequence b: none if its rows are not this kernel's.
+__device__ __forceinline__ int blocks_of(const PagedDev& g, int b) {
+  const int n = paged_rows(g, b).y;
+  if (n < g.least || n > g.most) return 0;
+  return (paged_len(g, b) + 15) / 16;
+}
+__device__ __forceinline__ int ranges_of(int64_t total, int n_cta) {  // a block for every warp at least
+  return (int)max((int64_t)1, min((int64_t)n_cta, (total + kWarps - 1) / kWarps));
+}
+
+template <int D, int NT>
+struct Shared {
+  float o[kWarps][8 * NT][D + 4];
+  float m[kWarps][8 * NT], l[kWarps][8 * NT];
+  uint2 q[NT][D / 16][32];  // query fragments: B operand of k-step s, lane (column, j)
+};
+
+template <int D, int NT>
+struct State {
+  float o[NT][D / 16][4];      // o[t][e][2 r + h]: column 8 t + 2 j + h, output column x D / 8 + 2 e + r
+  float m[NT][2], l[NT][2];    // log2 units; l: this thread's share
+};
+
+// One sequence's rows and pages as a warp sees them
+template <int D, int NT>
+struct Walk {
+  const AttnParams& p;
+  const __nv_bfloat16 *kp, *vp;  // this lane's columns of the KV head
+  int b, len, lane;
+  float cs;
+  int lim[NT][2];  // keys that this lane's columns see
+
+  __device__ __forceinline__ int page_of(int block) const {  // block below those of the sequence
+    return paged_page(p.paged, b, block * 16 / p.paged.page_size);
+  }
+  // blocks first, first + stride, .. (count of them)
+  template <int kAhead, typename Ready>
+  __device__ __forceinline__ void run(State<D, NT>& st, const uint2 (&q)[NT][D / 16][32], int first, int stride, int count, Ready ready) const {
+    if (count <= 0) {
+      ready();
+      return;
+    }
+    const int x = lane >> 2, j = lane & 3;
+    constexpr int kRegs = D / 8, kVRegs = D / 16;
+    uint32_t ka[kAhead][kRegs], kb[kAhead][kRegs], vr[kAhead][4][kVRegs];
+    // pages of the next 32 blocks, a lane each, and of the 32 after them
+    int pages = lane < count ? page_of(first + lane * stride) : 0, pages_next = 0;
+    auto page_at = [&](int t) {  // (asked in order)
+      if ((t & 31) == 0 && t > 0) pages = pages_next;
+      if ((t & 31) == 16) pages_next = (t & ~31) + 32 + lane < count ? page_of(first + ((t & ~31) + 32 + lane) * stride) : 0;
+      return __shfl_sync(0xffffffffu, pages, t & 31);
+    };
+    auto request = [&](int buf, int t, int page, bool keys) {
+      const int k0 = (first + t * stride) * 16, n = len - k0, slot = k0 % p.paged.page_size;
+      if (keys) {
+        const __nv_bfloat16* r = kp + (int64_t)page * p.ks.batch + (int64_t)slot * p.ks.token;
+        const __nv_bfloat16 *r0 = r + min(x, n - 1) * p.ks.token, *r1 = r + min(x + 8, n - 1) * p.ks.token;
+#pragma unroll
+        for (int c = 0; c < D / 64; ++c) {
+          load32(r0 + 64 * c, ka[buf] + 8 * c);
+          load32(r1 + 64 * c, kb[buf] + 8 * c);
+        }
+      } else {
+        const __nv_bfloat16* r = vp + (int64_t)page * p.vs.batch + (int64_t)slot * p.vs.token;
+#pragma unroll
+        for (int rr = 0; rr < 4; ++rr) {
+          const __nv_bfloat16* row = r + min(2 * j + (rr & 1) + (rr >> 1) * 8, n - 1) * p.vs.token;
+          if constexpr (D == 128) load32(row, vr[buf][rr]);
+          else load16(row, vr[buf][rr]);
+        }
+      }
+    };
+    int page[kAhead];
+#pragma unroll
+    for (int a = 0; a < kAhead; ++a) {
+      page[a] = 0;
+      if (a < count) {
+        page[a] = page_at(a);
+        request(a, a, page[a], true);
+        request(a, a, page[a], false);
+      }
+    }
+    ready();
+    auto block = [&](int t, int buf) {
+      const bool more = t + kAhead < count;
+      const int k0 = (first + t * stride) * 16;
+      float sc[NT][4];
+#pragma unroll
+      for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) sc[nt][i] = 0.f;
+#pragma unroll
+      for (int i = 0; i < D / 16; ++i)
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt) {
+          const uint2 f = q[nt][i][lane];
+          mma_16816(sc[nt], ka[buf][2 * i], kb[buf][2 * i], ka[buf][2 * i + 1], kb[buf][2 * i + 1], f.x, f.y);
+        }
+      int next = 0;
+      if (more) {
+        next = page_at(t + kAhead);
+        request(buf, t + kAhead, next, true);
+      }
+      uint32_t pa[NT][2], pb[NT][2];  // weights of keys x and x + 8, transposed; upper 16 bits and the rest
+      bool rescale = false;
+      float alpha[NT][2];
+#pragma unroll
+      for (int nt = 0; nt < NT; ++nt) {
+        float p0[2], p1[2];
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+          const float t0 = k0 + x < lim[nt][h] ? sc[nt][h] * cs : -INFINITY, t1 = k0 + x + 8 < lim[nt][h] ? sc[nt][2 + h] * cs : -INFINITY;
+          float mx = fmaxf(t0, t1);
+#pragma unroll
+          for (int o = 4; o < 32; o <<= 1) mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, o));
+          const float m_new = fmaxf(st.m[nt][h], mx), m_use = m_new == -INFINITY ? 0.f : m_new;
+          alpha[nt][h] = ex2f(st.m[nt][h] - m_use);  // 0 until something is seen
+          p0[h] = ex2f(t0 - m_use);
+          p1[h] = ex2f(t1 - m_use);
+          st.l[nt][h] = st.l[nt][h] * alpha[nt][h] + (p0[h] + p1[h]);
+          st.m[nt][h] = m_new;
+          rescale = rescale || alpha[nt][h] != 1.f;
+        }
+        auto rest = [](float w) { return w - __uint_as_float(__float_as_uint(w) & 0xffff0000u); };
+        pa[nt][0] = transpose8(__byte_perm(__float_as_uint(p0[0]), __float_as_uint(p0[1]), 0x7632));
+        pb[nt][0] = transpose8(__byte_perm(__float_as_uint(p1[0]), __float_as_uint(p1[1]), 0x7632));
+        pa[nt][1] = transpose8(pack2_bf16(rest(p0[0]), rest(p0[1])));
+        pb[nt][1] = transpose8(pack2_bf16(rest(p1[0]), rest(p1[1])));
+      }
+      if (__any_sync(0xffffffffu, rescale)) {
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+          for (int e = 0; e < D / 16; ++e)
+#pragma unroll
+            for (int c = 0; c < 4; ++c) st.o[nt][e][c] *= alpha[nt][c & 1];
+      }
+#pragma unroll
+      for (int e = 0; e < D / 16; ++e) {
+        const uint32_t a0 = __byte_perm(vr[buf][0][e], vr[buf][1][e], 0x5410), a1 = __byte_perm(vr[buf][0][e], vr[buf][1][e], 0x7632);
+        const uint32_t a2 = __byte_perm(vr[buf][2][e], vr[buf][3][e], 0x5410), a3 = __byte_perm(vr[buf][2][e], vr[buf][3][e], 0x7632);
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt) {
+          mma_16816(st.o[nt][e], a0, a1, a2, a3, pa[nt][0], pb[nt][0]);
+          mma_16816(st.o[nt][e], a0, a1, a2, a3, pa[nt][1], pb[nt][1]);
+        }
+      }
+      if (more) request(buf, t + kAhead, next, false);
+    };
+#pragma unroll 1
+    for (int t = 0; t < count; t += kAhead) {
+      block(t, 0);
+      if constexpr (kAhead == 2)
+        if (t + 1 < count) block(t + 1, 1);
+    }
+  }
+};
+
+template <int D, int NT>
+__device__ __forceinline__ void publish(Shared<D, NT>& sh, const State<D, NT>& st, int warp, int lane) {
+  const int x = lane >> 2, j = lane & 3;
+#pragma unroll
+  for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      float l = st.l[nt][h];
+#pragma unroll
+      for (int o = 4; o < 32; o <<= 1) l += __shfl_xor_sync(0xffffffffu, l, o);
+      const int col = 8 * nt + 2 * j + h;
+      if (x == 0) {
+        sh.m[warp][col] = st.m[nt][h];
+        sh.l[warp][col] = l;
+      }
+#pragma unroll
+      for (int e = 0; e < D / 16; ++e)
+        *reinterpret_cast<float2*>(&sh.o[warp][col][x * (D / 8) + 2 * e]) = make_float2(st.o[nt][e][h], st.o[nt][e][2 + h]);
+    }
+}
+// Output column c of column `col`: maximum, sum of weights and weighted sum over the warps
+template <int D, int NT>
+__device__ __forceinline__ void combine_warps(const Shared<D, NT>& sh, int col, int c, float& n, float& w, float& acc) {
+  n = -INFINITY;
+#pragma unroll
+  for (int i = 0; i < kWarps; ++i) n = fmaxf(n, sh.m[i][col]);
+  const float n_use = n == -INFINITY ? 0.f : n;
+  w = acc = 0.f;
+#pragma unroll
+  for (int i = 0; i < kWarps; ++i) {
+    const float f = ex2f(sh.m[i][col] - n_use);
+    w = fmaf(f, sh.l[i][col], w);
+    acc = fmaf(f, sh.o[i][col][c], acc);
+  }
+}
+
+// Output column c of (row, head) of column `col`: n and w in log2 units
+__device__ __forceinline__ void write_out(const AttnParams& p, const DecodeArgs& a, int row0, int item, int col, int c, float n, float w, float acc) {
+  const int r = col / a.Gi, row = row0 + r, head = item * a.Gi + col - r * a.Gi;
+  static_cast<__nv_bfloat16*>(p.o_out)[(int64_t)row * p.os.token + (int64_t)head * p.os.head + c] = __float2bfloat16_rn(w > 0.f ? acc / w : 0.f);
+  if (c == 0 && p.lse_out) p.lse_out[(int64_t)row * p.H + head] = w > 0.f ? n * 0.6931471805599453f + logf(w) : -INFINITY;
+}
+
+// The query fragments of item `item` of a sequence of `n` rows from row0 on, by warps 0 .. NT - 1
+template <int D, int NT>
+__device__ __forceinline__ void load_queries(Shared<D, NT>& sh, const AttnParams& p, const DecodeArgs& a, int row0, int n, int item, int warp, int lane) {
+  if (warp >= NT) return;
+  const int col = 8 * warp + (lane >> 2), j = lane & 3, r = col / a.Gi;
+  uint4 t[D / 32];
+#pragma unroll
+  for (int c = 0; c < D / 32; ++c) t[c] = make_uint4(0u, 0u, 0u, 0u);
+  if (r < n) {
+    const __nv_bfloat16* q = static_cast<const __nv_bfloat16*>(p.q) + (int64_t)(row0 + r) * p.qs.token + (int64_t)(item * a.Gi + col - r * a.Gi) * p.qs.head;
+#pragma unroll
+    for (int c = 0; c < D / 32; ++c) t[c] = __ldg(reinterpret_cast<const uint4*>(q + 64 * (c >> 1) + 16 * j + 8 * (c & 1)));
+  }
+#pragma unroll
+  for (int c = 0; c < D / 32; ++c) {
+    sh.q[warp][2 * c][lane] = make_uint2(t[c].x, t[c].y);
+    sh.q[warp][2 * c + 1][lane] = make_uint2(t[c].z, t[c].w);
+  }
+}
+
+template <int D, int NT>
+__device__ __forceinline__ Walk<D, NT> make_walk(const AttnParams& p, const DecodeArgs& a, int b, int row0, int n, int len, int item, int lane) {
+  const int x = lane >> 2, j = lane & 3, g = item * a.Gi / p.G;
+  Walk<D, NT> w{p, static_cast<const __nv_bfloat16*>(p.k) + (int64_t)g * p.ks.head + 16 * j,
+                static_cast<const __nv_bfloat16*>(p.v) + (int64_t)g * p.vs.head + x * (D / 8), b, len, lane, p.scale * 1.4426950408889634f, {}};
+#pragma unroll
+  for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      const int r = (8 * nt + 2 * j + h) / a.Gi;
+      w.lim[nt][h] = r < n ? paged_seen(p.paged, p.plan.causal, n, len, r, row0 + r) : 0;
+    }
+  return w;
+}
+template <int D, int NT>
+__device__ __forceinline__ void clear(State<D, NT>& st) {
+#pragma unroll
+  for (int nt = 0; nt < NT; ++nt) {
+#pragma unroll
+    for (int e = 0; e < D / 16; ++e)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) st.o[nt][e][i] = 0.f;
+    st.m[nt][0] = st.m[nt][1] = -INFINITY;
+    st.l[nt][0] = st.l[nt][1] = 0.f;
+  }
+}
+
+// ---- an item per cluster
+template <int D, int NT, int kAhead>
+__global__ void __launch_bounds__(kThreads, 3 - kAhead) paged_decode_cluster_kernel(const __grid_constant__ AttnParams p, const __grid_constant__ DecodeArgs a) {
+  extern __shared__ __align__(16) uint8_t smem[];
+  Shared<D, NT>& sh = *reinterpret_cast<Shared<D, NT>*>(smem);
+  __shared__ float s_o[8 * NT * D + kClusterMost], s_n[kClusterMost][8 * NT], s_w[kClusterMost][8 * NT];  // from each CTA of the cluster
+  const int rank = blockIdx.x, n_cta = a.n_cta, item = blockIdx.y, b = blockIdx.z;
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+  grid_go();
+  grid_wait();
+  asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");  // everyone has started: its shared memory may be written
+  const int2 rows = paged_rows(p.paged, b);
+  const bool mine = rows.y >= p.paged.least && rows.y <= p.paged.most;
+  if (rows.y > p.paged.most && p.alone && tid == 0) paged_report(p.paged.status, kBadRows, b, rows.y);
+  if (!mine) {  // (uniform for the cluster)
+    asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
+    return;
+  }
+  const int len = paged_len(p.paged, b), blocks = (len + 15) / 16, cols = rows.y * a.Gi;
+  load_queries(sh, p, a, rows.x, rows.y, item, warp, lane);
+  const Walk<D, NT> walk = make_walk<D, NT>(p, a, b, rows.x, rows.y, len, item, lane);
+  State<D, NT> st;
+  clear(st);
+  const int first = rank * kWarps + warp, stride = n_cta * kWarps;
+  walk.template run<kAhead>(st, sh.q, first, stride, first < blocks ? (blocks - first + stride - 1) / stride : 0, []() { __syncthreads(); });
+  publish(sh, st, warp, lane);
+  asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
+  __syncthreads();
+  // CTA r finishes outputs r * per_cta ..; every CTA sends it its share of them
+  const int outputs = cols * D, per_cta = (outputs + n_cta - 1) / n_cta;
+  auto send = [&](const float* local, int to, float v) {
+    uint32_t addr;
+    asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(addr) : "r"((uint32_t)__cvta_generic_to_shared(local)), "r"(to));
+    asm volatile("st.shared::cluster.f32 [%0], %1;" ::"r"(addr), "f"(v) : "memory");
+  };
+  for (int i = tid; i < outputs; i += kThreads) {
+    float n, w, acc;
+    combine_warps(sh, i / D, i % D, n, w, acc);
+    const int to = i / per_cta;
+    send(&s_o[rank * per_cta + i - to * per_cta], to, acc);
+    if (i % D < n_cta) {
+      send(&s_n[rank][i / D], i % D, n);
+      send(&s_w[rank][i / D], i % D, w);
+    }
+  }
+  asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
+  const int here = min(per_cta, outputs - rank * per_cta);
+  for (int o = tid; o < here; o += kThreads) {
+    const int col = (rank * per_cta + o) / D, c = (rank * per_cta + o) % D;
+    float n = -INFINITY, w = 0.f, acc = 0.f;
+    for (int r = 0; r < n_cta; ++r) n = fmaxf(n, s_n[r][col]);
+    const float n_use = n == -INFINITY ? 0.f : n;
+#pragma unroll 4
+    for (int r = 0; r < n_cta; ++r) {
+      const float f = ex2f(s_n[r][col] - n_use);
+      w = fmaf(f, s_w[r][col], w);
+      acc = fmaf(f, s_o[r * per_cta + o], acc);
+    }
+    write_out(p, a, rows.x, item, col, c, n, w, acc);
+  }
+}
+
+// ---- ranges of equal length
+template <int D, int NT, int kAhead>
+__global__ void __launch_bounds__(kThreads, 3 - kAhead) paged_decode_ranges_kernel(const __grid_constant__ AttnParams p, const __grid_constant__ DecodeArgs a) {
+  extern __shared__ __align__(16) uint8_t smem[];
+  Shared<D, NT>& sh = *reinterpret_cast<Shared<D, NT>*>(smem);
+  __shared__ int s_group[kMaxGroups + 1];  // blocks (of one item) of the groups of 32 sequences before
+  __shared__ RangeStart s_start;
+  const PagedDev& g = p.paged;
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, cta = blockIdx.x;
+  grid_go();
+  grid_wait();
+  const int groups = (g.batch + 31) / 32;
+  for (int i = warp; i < groups; i += kWarps) {
+    const int b = i * 32 + lane, n = b < g.batch ? blocks_of(g, b) : 0;
+    const int sum = __reduce_add_sync(0xffffffffu, n);
+    if (lane == 0) s_group[i] = sum;
+    if (cta == 0 && b < g.batch) {
+      const int rows = paged_rows(g, b).y;
+      if (rows > g.most && p.alone) paged_report(g.status, kBadRows, b, rows);  // nobody else takes it
+    }
+    // rows over an empty cache
+    if (b < g.batch && n == 0 && b % a.n_cta == cta) {
+      const int2 rows = paged_rows(g, b);
+      if (rows.y >= g.least && rows.y <= g.most)
+        for (int64_t e = 0; e < (int64_t)rows.y * p.H; ++e) {
+          const int64_t row = rows.x + e / p.H, head = e % p.H;
+          uint4* o = reinterpret_cast<uint4*>(static_cast<__nv_bfloat16*>(p.o_out) + row * p.os.token + head * p.os.head);
+          for (int c = 0; c < D / 8; ++c) o[c] = make_uint4(0u, 0u, 0u, 0u);
+          if (p.lse_out) p.lse_out[row * p.H + head] = -INFINITY;
+        }
+    }
+  }
+  __syncthreads();
+  if (warp == 0) {
+    int before = 0;
+    for (int i0 = 0; i0 < groups; i0 += 32) {
+      const int i = i0 + lane, n = i < groups ? s_group[i] : 0;
+      int incl = n;
+#pragma unroll
+      for (int o = 1; o < 32; o <<= 1) {
+        const int u = __shfl_up_sync(0xffffffffu, incl, o);
+        if (lane >= o) incl += u;
+      }
+      if (i < groups) s_group[i] = before + incl - n;
+      before += __shfl_sync(0xffffffffu, incl, 31);
+    }
+    if (lane == 0) s_group[groups] = before;
+    const int64_t total = (int64_t)before * a.items;
+    const int n_ranges = ranges_of(total, a.n_cta);
+    RangeStart r = {-1, 0, 0, 0, total};
+    if (cta < n_ranges && total > 0) {
+      const int64_t u = total * cta / n_ranges;
+      const int at = (int)(u / a.items);  // some block of the sequence (sequences have items times their blocks)
+      int lo = 0, hi = groups - 1;
+      __syncwarp();
+      while (lo < hi) {
+        const int mid = (lo + hi + 1) >> 1;
+        if (s_group[mid] <= at) lo = mid;
+        else hi = mid - 1;
+      }
+      const int b = lo * 32 + lane, n = b < g.batch ? blocks_of(g, b) : 0;
+      int incl = n;
+#pragma unroll
+      for (int o = 1; o < 32; o <<= 1) {
+        const int t = __shfl_up_sync(0xffffffffu, incl, o);
+        if (lane >= o) incl += t;
+      }
+      const uint32_t past = __ballot_sync(0xffffffffu, (int64_t)(s_group[lo] + incl) * a.items > u);
+      const int who = __ffs(past) - 1;  // the group holds block `at`
+      const int nb = __shfl_sync(0xffffffffu, n, who), start = s_group[lo] + __shfl_sync(0xffffffffu, incl, who) - nb;
+      const int64_t off = u - (int64_t)start * a.items;
+      r.b = lo * 32 + who;
+      r.item = (int)(off / nb);
+      r.before = (int)(off - (int64_t)r.item * nb);
+      r.blocks = nb;
+    }
+    if (lane == 0) {
+      s_start = r;
+      a.starts[cta] = r;
+    }
+  }
+  __syncthreads();
+  const RangeStart r = s_start;
+  if (r.b < 0) return;
+  const int n_ranges = ranges_of(r.total, a.n_cta);
+  int64_t left = r.total * (cta + 1) / n_ranges - r.total * cta / n_ranges;
+  int b = r.b, item = r.item, s0 = r.before, blocks = r.blocks;
+  while (left > 0) {
+    const int s1 = (int)min((int64_t)blocks, s0 + left);
+    const int2 rows = paged_rows(g, b);
+    const int len = paged_len(g, b), cols = rows.y * a.Gi;
+    load_queries(sh, p, a, rows.x, rows.y, item, warp, lane);
+    const Walk<D, NT> walk = make_walk<D, NT>(p, a, b, rows.x, rows.y, len, item, lane);
+    State<D, NT> st;
+    clear(st);
+    const int first = s0 + warp;
+    walk.template run<kAhead>(st, sh.q, first, kWarps, first < s1 ? (s1 - first + kWarps - 1) / kWarps : 0, []() { __syncthreads(); });
+    publish(sh, st, warp, lane);
+    __syncthreads();
+    const bool whole = s0 == 0 && s1 == blocks;
+    float* part = a.partials + (int64_t)(cta * 2 + (s0 > 0 ? 0 : 1)) * (8 * NT * (D + 2));
+    for (int i = tid; i < cols * D; i += kThreads) {
+      const int col = i / D, c = i % D;
+      float n, w, acc;
+      combine_warps(sh, col, c, n, w, acc);
+      if (whole) {
+        write_out(p, a, rows.x, item, col, c, n, w, acc);
+      } else {
+        part[i] = acc;
+        if (c == 0) {
+          part[8 * NT * D + col] = n;
+          part[8 * NT * (D + 1) + col] = w;
+        }
+      }
+    }
+    left -= s1 - s0;
+    s0 = 0;
+    if (++item == a.items) {  // the next sequence that has blocks
+      item = 0;
+      do ++b;
+      while (b < g.batch && (blocks = blocks_of(g, b)) == 0);
+      if (b >= g.batch) break;
+    }
+    __syncthreads();  // the shares and queries have been read
+  }
+}
+
+// CTA i adds up the item that is cut for the first time where range i + 1 starts.
+template <int D, int NT>
+__global__ void __launch_bounds__(kThreads) paged_decode_join_kernel(const __grid_constant__ AttnParams p, const __grid_constant__ DecodeArgs a) {
+  grid_go();
+  grid_wait();
+  const int at = blockIdx.x + 1;
+  const RangeStart r = a.starts[at];
+  if (r.b < 0 || r.before == 0) return;
+  const int n_ranges = ranges_of(r.total, a.n_cta);
+  auto start = [&](int i) { return r.total * i / n_ranges; };
+  const int64_t u0 = start(at) - r.before, u1 = u0 + r.blocks;  // the item
+  if (start(at - 1) > u0) return;  // cut before
+  int last = at;  // the last range that has a part of it
+  while (last + 1 < n_ranges && start(last + 1) < u1) ++last;
+  const int2 rows = paged_rows(p.paged, r.b);
+  const int cols = rows.y * a.Gi;
+  auto part = [&](int i) { return a.partials + (int64_t)(i * 2 + (i == at - 1 ? 1 : 0)) * (8 * NT * (D + 2)); };
+  for (int i = threadIdx.x; i < cols * D; i += kThreads) {
+    const int col = i / D, c = i % D;
+    float n = -INFINITY, w = 0.f, acc = 0.f;
+    for (int k = at - 1; k <= last; ++k) n = fmaxf(n, __ldcg(part(k) + 8 * NT * D + col));
+    const float n_use = n == -INFINITY ? 0.f : n;
+    for (int k = at - 1; k <= last; ++k) {
+      const float* q = part(k);
+      const float f = ex2f(__ldcg(q + 8 * NT * D + col) - n_use);
+      w = fmaf(f, __ldcg(q + 8 * NT * (D + 1) + col), w);
+      acc = fmaf(f, __ldcg(q + i), acc);
+    }
+    write_out(p, a, rows.x, r.item, col, c, n, w, acc);
+  }
+}
+
+template <typename F>
+cudaError_t with_shape(int d, int columns, F f) {
+  using I1 = std::integral_constant<int, 1>;
+  using I2 = std::integral_constant<int, 2>;
+  if (d == 128) {
+    using D = std::integral_constant<int, 128>;
+    return columns <= 8 ? f(D(), I1()) : f(D(), I2());
+  }
+  using D = std::integral_constant<int, 64>;
+  return columns <= 8 ? f(D(), I1()) : f(D(), I2());
+}
+
+int ranges_cta(int d, int columns) { return d == 128 && columns > 8 ? 148 : 296; }  // CTAs that are resident at a time
+int64_t decode_items(const AttnParams& p) { return (int64_t)p.paged.batch * (p.H / paged_decode_heads(p)); }
+int cluster_size(const AttnParams& p) {  // 0: ranges
+  const int64_t items = decode_items(p);
+  if (items > 32) return 0;
+  const int64_t blocks = ((int64_t)p.paged.max_pages * p.paged.page_size + 15) / 16;
+  const int64_t most = std::min<int64_t>(items <= 7 ? kClusterMost : 10, (blocks + kWarps - 1) / kWarps);
+  return (int)std::max<int64_t>(1, std::min<int64_t>(256 / items, most));
+}
+
+}  // namespace
+
+// Heads of an item: the largest divisor of the group that fits the columns.
+int paged_decode_heads(const AttnParams& p) {
+  for (int n = std::min(16, p.G); n > 1; --n)
+    if (p.G % n == 0) return n;
+  return 1;
+}
+int paged_decode_rows(const AttnParams& p) { return 16 / paged_decode_heads(p); }
+
+size_t paged_decode_ws_bytes(const AttnParams& p, int rows) {
+  if (cluster_size(p) > 0) return 0;
+  const int columns = rows * paged_decode_heads(p) <= 8 ? 8 : 16, n = ranges_cta(p.d, columns);
+  return (size_t)n * (2 * columns * (p.d + 2) * 4 + sizeof(RangeStart));
+}
+
+cudaError_t launch_paged_decode(const AttnParams& p, int rows, void* workspace, cudaStream_t stream) {
+  DecodeArgs a = {};
+  a.Gi = paged_decode_heads(p);
+  a.items = p.H / a.Gi;
+  const int columns = rows * a.Gi, cluster = cluster_size(p);
+  TimedLaunch timed(stream);
+  return with_shape(p.d, columns, [&](auto d, auto nt) {
+    constexpr int D = decltype(d)::value, NT = decltype(nt)::value;
+    constexpr int smem = (int)sizeof(Shared<D, NT>);
+    if (cluster > 0) {
+      constexpr int kAhead = 2;
+      auto kernel = paged_decode_cluster_kernel<D, NT, kAhead>;
+      cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
+      if (e == cudaSuccess && cluster > 8) e = cudaFuncSetAttribute(kernel, cudaFuncAttributeNonPortableClusterSizeAllowed, 1);
+      if (e != cudaSuccess) return e;
+      a.n_cta = cluster;
+      return launch_dependent(kernel, dim3(cluster, a.items, p.paged.batch), kThreads, smem, cluster, true, stream, p, a);
+    }
+    constexpr int kAhead = D == 128 && NT == 2 ? 2 : 1;
+    a.n_cta = ranges_cta(p.d, columns);
+    a.starts = static_cast<RangeStart*>(workspace);
+    a.partials = reinterpret_cast<float*>(a.starts + a.n_cta);
+    auto kernel = paged_decode_ranges_kernel<D, NT, kAhead>;
+    cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
+    if (e != cudaSuccess) return e;
+    e = launch_dependent(kernel, dim3(a.n_cta), kThreads, smem, 1, true, stream, p, a);
+    if (e != cudaSuccess) return e;
+    return launch_dependent(paged_decode_join_kernel<D, NT>, dim3(a.n_cta - 1), kThreads, 0, 1, true, stream, p, a);
+  });
+}
+
+}  // namespace cascade
