@@ -521,7 +521,7 @@ cudaError_t with_shape(int d, int columns, F f) {
   return columns <= 8 ? f(D(), I1()) : f(D(), I2());
 }
 
-int ranges_cta(int d, int columns) { return d == 128 && columns > 8 ? 148 : 296; }  // CTAs that are resident at a time
+int ranges_cta(int d, int) { return d == 128 ? 148 : 296; }  // CTAs that are resident at a time
 int64_t decode_items(const AttnParams& p) { return (int64_t)p.paged.batch * (p.H / paged_decode_heads(p)); }
 int cluster_size(const AttnParams& p) {  // 0: ranges
   const int64_t items = decode_items(p);
@@ -565,7 +565,7 @@ cudaError_t launch_paged_decode(const AttnParams& p, int rows, void* workspace, 
       a.n_cta = cluster;
       return launch_dependent(kernel, dim3(cluster, a.items, p.paged.batch), kThreads, smem, cluster, true, stream, p, a);
     }
-    constexpr int kAhead = D == 128 && NT == 2 ? 2 : 1;
+    constexpr int kAhead = D == 128 ? 2 : 1;
     a.n_cta = ranges_cta(p.d, columns);
     a.starts = static_cast<RangeStart*>(workspace);
     a.partials = reinterpret_cast<float*>(a.starts + a.n_cta);
