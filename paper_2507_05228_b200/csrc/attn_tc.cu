@@ -301,8 +301,14 @@ __global__ void __launch_bounds__(kThreads, 1) attn_tc_kernel(const __grid_const
   }
   // A gather right before this grid runs after all that came before it, and writes only what the loaders read: they wait
   // for it.
-  grid_go();
-  if (!after_gather) grid_wait();
+  // kPaged: what starts early may be the decode kernel of the same call, which reads what came before without waiting for this grid.
+  if constexpr (kPaged) {
+    grid_wait();
+    grid_go();
+  } else {
+    grid_go();
+    if (!after_gather) grid_wait();
+  }
   const int map = kPaged || pl.n_maps == 1 ? 0 : b;
   const int h0 = hg * Gp;  // first of the Gp stacked heads
   const int per_kv = p.G >> lg;  // head groups per KV head

@@ -26,6 +26,7 @@ struct Api {
   decltype(&cascade_decode_step_rope) decode_step_rope;
   decltype(&cascade_attn_decode_static) decode_static;
   decltype(&cascade_plan_advance) plan_advance;
+  decltype(&cascade_rope_table_scaled) rope_table_scaled;
   decltype(&cascade_rope_rows) rope_rows;
   decltype(&cascade_paged_append) paged_append;
   decltype(&cascade_attn_paged) attn_paged;
@@ -388,6 +389,25 @@ struct Pages {
   }
 };
 
+double real(PyObject* o) {
+  const double v = PyFloat_AsDouble(o);
+  if (v == -1.0 && PyErr_Occurred()) throw PyFailure();
+  return v;
+}
+// (n_positions, rot_dim, base, kind, factor, original_positions, low, high, attention, table) -> table
+PyObject* rope_table_scaled(PyObject* const* a) {
+  const long long n = integer(a[0]), rot = integer(a[1]);
+  need(n > INT32_MIN && n <= INT32_MAX && rot > INT32_MIN && rot <= INT32_MAX, "n_positions and rot_dim are 32-bit numbers");
+  const int32_t kind = (int32_t)integer(a[3]);
+  const double base = real(a[2]), factor = real(a[4]), original = real(a[5]), low = real(a[6]), high = real(a[7]), attention = real(a[8]);
+  const at::Tensor& table = here(a[9]);
+  auto* tp = static_cast<float*>(table.data_ptr());
+  void* st = stream();
+  check(unlocked([&] { return api.rope_table_scaled((int32_t)n, (int32_t)rot, base, kind, factor, original, low, high, attention, tp, st); }));
+  Py_INCREF(a[9]);
+  return a[9];
+}
+
 // (x, positions, rope_table, interleaved, out or None) -> out
 PyObject* rope_rows(PyObject* const* a) {
   const at::Tensor &x = here(a[0]), &positions = here(a[1]), &table = here(a[2]);
@@ -613,6 +633,7 @@ PyObject* load(PyObject*, PyObject* args) {
   find(api.decode_step_rope, "cascade_decode_step_rope");
   find(api.decode_static, "cascade_attn_decode_static");
   find(api.plan_advance, "cascade_plan_advance");
+  find(api.rope_table_scaled, "cascade_rope_table_scaled");
   find(api.rope_rows, "cascade_rope_rows");
   find(api.paged_append, "cascade_paged_append");
   find(api.attn_paged, "cascade_attn_paged");
@@ -640,6 +661,7 @@ PyMethodDef methods[] = {
     {"decode_step_rope", fast<12, decode_step_rope>(), METH_FASTCALL, nullptr},
     {"attn_decode_static", fast<7, attn_decode_static>(), METH_FASTCALL, nullptr},
     {"plan_advance", fast<2, plan_advance>(), METH_FASTCALL, nullptr},
+    {"rope_table_scaled", fast<10, rope_table_scaled>(), METH_FASTCALL, nullptr},
     {"rope_rows", fast<5, rope_rows>(), METH_FASTCALL, nullptr},
     {"paged_append", fast<12, paged_append>(), METH_FASTCALL, nullptr},
     {"attn_paged", fast<13, attn_paged>(), METH_FASTCALL, nullptr},

@@ -2,6 +2,8 @@
 // address, and the words that they report to.
 #pragma once
 
+#include <limits.h>
+
 #include "cascade_internal.cuh"
 
 namespace cascade {
@@ -55,27 +57,25 @@ __device__ __forceinline__ int paged_seen(const PagedDev& g, bool causal, int n,
   return causal ? max(0, len - n + i + 1) : len;
 }
 
-// Sequence and tile of tile number t, of those of `per_tile` rows each that the sequences of least .. most rows have, one sequence
-// after another; the last tile of a sequence (which sees most) comes first.  {sequence, tile}, or {-1, 0} past the last.  All lanes
-// of a warp.
+// Sequence and tile of tile number t, of those of `per_tile` rows each that the sequences of least .. most rows have: of 32
+// sequences at a time the one with the longest cache first, and of a sequence its last tile (which sees most), so that the last
+// tiles to start are short ones.  {sequence, tile}, or {-1, 0} past the last.  All lanes of a warp.
 __device__ __forceinline__ int2 paged_tile(const PagedDev& g, int t, int per_tile, int lane) {
   int before = 0;
   for (int b0 = 0; b0 < g.batch; b0 += 32) {
     const int b = b0 + lane;
     const int n = b < g.batch ? paged_rows(g, b).y : 0;
     const int tiles = n >= g.least && n <= g.most ? (n + per_tile - 1) / per_tile : 0;
-    int incl = tiles;
-#pragma unroll
-    for (int o = 1; o < 32; o <<= 1) {
-      const int u = __shfl_up_sync(0xffffffffu, incl, o);
-      if (lane >= o) incl += u;
-    }
-    const int total = __shfl_sync(0xffffffffu, incl, 31);
+    const int total = __reduce_add_sync(0xffffffffu, tiles);
     if (t < before + total) {
-      const uint32_t past = __ballot_sync(0xffffffffu, before + incl > t);
-      const int who = __ffs(past) - 1;
-      const int end = before + __shfl_sync(0xffffffffu, incl, who);
-      return make_int2(b0 + who, end - 1 - t);
+      const int len = tiles > 0 ? __ldg(g.kv_len + b) : INT_MIN;
+      int first = before;  // tiles of the sequences that come before this lane's
+      for (int j = 0; j < min(32, g.batch - b0); ++j) {
+        const int other = __shfl_sync(0xffffffffu, len, j), n_other = __shfl_sync(0xffffffffu, tiles, j);
+        if (other > len || (other == len && j < lane)) first += n_other;
+      }
+      const int who = __ffs(__ballot_sync(0xffffffffu, t >= first && t < first + tiles)) - 1;
+      return make_int2(b0 + who, __shfl_sync(0xffffffffu, first + tiles, who) - 1 - t);
     }
     before += total;
   }

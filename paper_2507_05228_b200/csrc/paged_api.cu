@@ -362,15 +362,15 @@ cascade_status_t cascade_attn_paged(cascade_dtype_t dtype, int32_t batch, int32_
   const PagedRoute r = paged_route(p, max_rows);
   if (r.tiles && !paged_tc_takes(p)) return launched(launch_paged_alu(p, dtype, workspace, st), fn);
   cudaError_t e = cudaSuccess;
-  if (r.rows > 0) {
-    AttnParams few = p;
-    few.paged.most = r.rows;
-    few.alone = !r.tiles;
-    e = launch_paged_decode(few, r.rows, workspace, st);
+  if (r.tiles) {
+    AttnParams many = p;
+    many.paged.least = r.rows + 1;
+    e = launch_paged_tc(many, st);
   }
-  if (e == cudaSuccess && r.tiles) {
-    p.paged.least = r.rows + 1;
-    e = launch_paged_tc(p, st);
+  if (e == cudaSuccess && r.rows > 0) {
+    p.paged.most = r.rows;
+    p.alone = !r.tiles;
+    e = launch_paged_decode(p, r.rows, workspace, st);
   }
   return launched(e, fn);
 }

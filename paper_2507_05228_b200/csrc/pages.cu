@@ -5,8 +5,12 @@
 // ones, hand them out), each of which needs all of the one before: latency, not bytes.  One cluster of CTAs does the whole chain
 // in one launch, with the cluster's hardware barrier between the steps and the few totals that the CTAs exchange in distributed
 // shared memory.  A page is free when no sequence holds it, so the holders are counted anew every time and no list of free pages
-// has to be kept.  No list is written either: whoever ranks a free page looks up who takes the page of that rank.
+// has to be kept.  No list is written either: whoever ranks a free page looks up who takes the page of that rank.  Where the holders
+// fit in the shared memory of one CTA (kOne), that CTA does it alone, without a barrier or a trip to L2 between the steps (64
+// sequences, 1800 pages: fork 10 -> us, compaction -> ).
 // Copying is bound by HBM: twice the bytes of the pages.
+#include <limits.h>
+
 #include "paged.cuh"
 
 namespace cascade {
@@ -14,7 +18,7 @@ namespace cascade {
 namespace {
 
 constexpr int kPagesThreads = 1024, kMaxPagesCluster = 16;
-constexpr int kMaxForkSeqs = 8192;  // whose places fit in shared memory
+constexpr int kMaxForkSeqs = 8192;  // six words each in shared memory
 
 // (all threads of the cluster; orders their accesses to global and shared memory)
 __device__ __forceinline__ void cluster_sync() {
@@ -68,25 +72,54 @@ __device__ __forceinline__ void rank_pages(int first, int end, int rank0, int* s
   }
 }
 
+// Holders of the pages: in p.refs, for all CTAs of the cluster, or (kOne) in shared memory until the end.
+template <bool kOne>
+struct Holders {
+  int* refs;
+  __device__ __forceinline__ int get(int page) const { return kOne ? refs[page] : __ldcg(refs + page); }
+};
+template <bool kOne>
+__device__ __forceinline__ void sync_all() {
+  if constexpr (kOne) __syncthreads();
+  else cluster_sync();
+}
+
 // Entries of row `row` of the table that are pages of it; a bad length has none.
 __device__ __forceinline__ int pages_of(int rows, const PagesParams& p) {
   return rows < 0 || rows > (int64_t)p.width * p.page_size ? -1 : (rows + p.page_size - 1) / p.page_size;
 }
 
+// f(sequence, column, entry) for this thread's share of the table
+template <typename F>
+__device__ __forceinline__ void for_entries(int n, int width, int64_t mine, int all, F f) {
+  const int64_t entries = (int64_t)n * width;
+  if (entries <= INT_MAX - all) {  // (a 64-bit division takes as long as a trip to L2)
+#pragma unroll 4
+    for (int e = (int)mine; e < (int)entries; e += all) f(e / width, e % width, (int64_t)e);
+  } else {
+    for (int64_t e = mine; e < entries; e += all) f((int)(e / width), (int)(e % width), e);
+  }
+}
+
+template <bool kOne>
 __global__ void __launch_bounds__(kPagesThreads) pages_fork_kernel(const __grid_constant__ PagesParams p) {
   extern __shared__ int s_dyn[];
-  __shared__ int s_warp[32], s_all[kMaxPagesCluster], s_bad, s_long, s_carry;
+  __shared__ int s_warp[32], s_all[kMaxPagesCluster], s_bad, s_long, s_carry, s_ids;
   const int n = p.n_seqs, P = p.page_size;
-  int* s_at = s_dyn;          // pages that the sequences before take
-  int* s_last = s_dyn + n;    // page that the sequence goes on writing, -1: none
+  int* s_at = s_dyn;           // pages that the sequences before take
+  int* s_last = s_dyn + n;     // page that the sequence goes on writing, -1: none
   int* s_had = s_dyn + 2 * n;  // rows it has
-  const int n_cta = gridDim.x, rank = blockIdx.x, tid = threadIdx.x;
+  int* s_src = s_dyn + 3 * n;  // the sequence it continues
+  int* s_add = s_dyn + 4 * n;  // rows it gets
+  int* s_own = s_dyn + 5 * n;  // 1: it gets a copy of that page
+  const Holders<kOne> holders{kOne ? s_dyn + 6 * n : p.refs};
+  const int n_cta = kOne ? 1 : gridDim.x, rank = kOne ? 0 : blockIdx.x, tid = threadIdx.x;
   const int gt = rank * kPagesThreads + tid, all = n_cta * kPagesThreads;
   grid_go();
   grid_wait();
-  if (tid == 0) s_bad = s_long = s_carry = 0;
+  if (tid == 0) s_bad = s_long = s_carry = s_ids = 0;
   __syncthreads();
-  for (int i = gt; i < p.n_pages; i += all) p.refs[i] = 0;
+  for (int i = gt; i < p.n_pages; i += all) holders.refs[i] = 0;
   if (gt < 4) p.report[gt] = 0;
   for (int i = tid; i < n; i += kPagesThreads) {
     const int src = __ldg(p.source + i), add = __ldg(p.add + i);
@@ -105,44 +138,42 @@ __global__ void __launch_bounds__(kPagesThreads) pages_fork_kernel(const __grid_
     if ((int64_t)had + max(add, 0) > (int64_t)p.width * P) atomicAdd(&s_long, 1);
     s_had[i] = had;
     s_last[i] = last;
+    s_src[i] = src;
+    s_add[i] = max(0, add);
   }
-  cluster_sync();
+  sync_all<kOne>();
   // holders of every page
-  for (int64_t e = gt; e < (int64_t)n * p.width; e += all) {
-    const int i = (int)(e / p.width), c = (int)(e - (int64_t)i * p.width);
+  for_entries(n, p.width, gt, all, [&](int i, int c, int64_t) {
     if ((int64_t)c * P < s_had[i]) {
-      const int page = __ldg(p.table_in + (int64_t)__ldg(p.source + i) * p.width + c);
-      if ((unsigned)page < (unsigned)p.n_pages) atomicAdd(p.refs + page, 1);
-      else atomicAdd(p.report + 2, 1);
+      const int page = __ldg(p.table_in + (int64_t)s_src[i] * p.width + c);
+      if ((unsigned)page < (unsigned)p.n_pages) atomicAdd(holders.refs + page, 1);
+      else atomicAdd(kOne ? &s_ids : p.report + 2, 1);
     }
-  }
-  cluster_sync();
+  });
+  sync_all<kOne>();
   // A sequence that goes on writing a page that others hold, too, gets a copy of its own: except the first of them where all
   // would write it (they leave, it stays alone with it).  A reader among them sees the rows that it has and no more, but may write
-  // there itself one day.
-  for (int i = gt; i < n; i += all) {
+  // there itself one day.  (Every CTA works this out for all sequences: few have such a page.)
+  for (int i = tid; i < n; i += kPagesThreads) {
     const int last = s_last[i];
-    bool copied = false;
+    bool own = false;
     if ((unsigned)last < (unsigned)p.n_pages) {
-      const int holders = __ldcg(p.refs + last);
-      if (holders > 1) {
+      const int held = holders.get(last);
+      if (held > 1) {
         int writers = 0, first = n;
         for (int j = n - 1; j >= 0; --j)
           if (s_last[j] == last) {
             ++writers;
             first = j;
           }
-        copied = !(writers == holders && first == i);
+        own = !(writers == held && first == i);
       }
     }
-    *reinterpret_cast<int2*>(p.pairs + 2 * i) = make_int2(copied ? last : -1, -1);
+    s_own[i] = own ? 1 : 0;
   }
-  cluster_sync();
+  __syncthreads();
   // pages that every sequence takes, and how many those before it take
-  auto takes = [&](int i) {
-    const int64_t rows = (int64_t)s_had[i] + max(0, __ldg(p.add + i));
-    return (int)((rows + P - 1) / P) - (s_had[i] + P - 1) / P + (__ldcg(p.pairs + 2 * i) >= 0 ? 1 : 0);
-  };
+  auto takes = [&](int i) { return (int)(((int64_t)s_had[i] + s_add[i] + P - 1) / P) - (s_had[i] + P - 1) / P + s_own[i]; };
   for (int i0 = 0; i0 < n; i0 += kPagesThreads) {
     const int i = i0 + tid, mine = i < n ? takes(i) : 0, lane = tid & 31;
     int incl = mine;
@@ -162,38 +193,41 @@ __global__ void __launch_bounds__(kPagesThreads) pages_fork_kernel(const __grid_
   }
   const int need = s_carry, chunk = (p.n_pages + n_cta - 1) / n_cta;
   const int first = min(p.n_pages, rank * chunk), end = min(p.n_pages, first + chunk);
-  auto is_free = [&](int page) { return __ldcg(p.refs + page) == 0; };
-  const int n_free_here = count_pages(first, end, s_warp, is_free);
-  if (tid == 0) tell_cluster(s_all, rank, n_cta, n_free_here);
-  cluster_sync();
-  int n_free = 0, rank0 = 0;
-  for (int r = 0; r < n_cta; ++r) {
-    if (r < rank) rank0 += s_all[r];
-    n_free += s_all[r];
-  }
-  const int bad_pages = __ldcg(p.report + 2);
-  if (s_bad + s_long + bad_pages > 0 || need > n_free) {  // nothing is done (the same decision in every CTA)
+  auto is_free = [&](int page) { return holders.get(page) == 0; };
+  int n_free = count_pages(first, end, s_warp, is_free), rank0 = 0;
+  if constexpr (!kOne) {
+    if (tid == 0) tell_cluster(s_all, rank, n_cta, n_free);
     cluster_sync();
-    for (int i = gt; i < p.n_pages; i += all) p.refs[i] = 0;
+    n_free = 0;
+    for (int r = 0; r < n_cta; ++r) {
+      if (r < rank) rank0 += s_all[r];
+      n_free += s_all[r];
+    }
+  }
+  const int bad_ids = kOne ? s_ids : __ldcg(p.report + 2);
+  if (s_bad + s_long + bad_ids > 0 || need > n_free) {  // nothing is done (the same decision in every CTA)
+    sync_all<kOne>();
+    for (int i = gt; i < p.n_pages; i += all) holders.refs[i] = 0;
     for (int i = gt; i < n; i += all) {
       *reinterpret_cast<int2*>(p.pairs + 2 * i) = make_int2(-1, -1);
       p.kv_out[i] = __ldg(p.kv_in + i);
     }
-    cluster_sync();
-    for (int64_t e = gt; e < (int64_t)n * p.width; e += all) {
-      const int i = (int)(e / p.width), page = __ldg(p.table_in + e);
+    sync_all<kOne>();
+    for_entries(n, p.width, gt, all, [&](int i, int c, int64_t e) {
+      const int page = __ldg(p.table_in + e);
       p.table_out[e] = page;
-      if ((int)(e - (int64_t)i * p.width) < pages_of(__ldg(p.kv_in + i), p) && (unsigned)page < (unsigned)p.n_pages)
-        atomicAdd(p.refs + page, 1);
-    }
-    cluster_sync();
+      if (c < pages_of(__ldg(p.kv_in + i), p) && (unsigned)page < (unsigned)p.n_pages) atomicAdd(holders.refs + page, 1);
+    });
+    sync_all<kOne>();
     const int left = count_pages(first, end, s_warp, is_free);
     if (tid == 0) atomicAdd(p.report + 3, left);
     if (gt == 0) {
       p.report[0] = max(0, need - n_free);
       p.report[1] = s_long;
-      p.report[2] = bad_pages + s_bad;
+      p.report[2] = bad_ids + s_bad;
     }
+    if constexpr (kOne)
+      for (int i = tid; i < p.n_pages; i += kPagesThreads) p.refs[i] = holders.refs[i];
     return;
   }
   // The page of rank r goes to the last sequence whose first rank is not above r (one that takes none shares its first rank with
@@ -206,108 +240,124 @@ __global__ void __launch_bounds__(kPagesThreads) pages_fork_kernel(const __grid_
       if (s_at[mid] <= r) lo = mid;
       else hi = mid - 1;
     }
-    const int off = r - s_at[lo], old = (s_had[lo] + P - 1) / P;
-    const bool copied = __ldcg(p.pairs + 2 * lo) >= 0;
-    if (copied && off == 0) p.pairs[2 * lo + 1] = page;
-    p.table_out[(int64_t)lo * p.width + old + off - (copied ? 1 : 0)] = page;
-    p.refs[page] = 1;
+    const int off = r - s_at[lo], old = (s_had[lo] + P - 1) / P, own = s_own[lo];
+    if (own && off == 0) *reinterpret_cast<int2*>(p.pairs + 2 * lo) = make_int2(s_last[lo], page);
+    p.table_out[(int64_t)lo * p.width + old + off - own] = page;
+    holders.refs[page] = 1;
   });
-  for (int64_t e = gt; e < (int64_t)n * p.width; e += all) {
-    const int i = (int)(e / p.width), c = (int)(e - (int64_t)i * p.width), had = s_had[i];
+  for_entries(n, p.width, gt, all, [&](int i, int c, int64_t e) {
+    const int had = s_had[i];
     if ((int64_t)c * P < had) {
-      if (s_last[i] >= 0 && c == had / P && __ldcg(p.pairs + 2 * i) >= 0) atomicSub(p.refs + s_last[i], 1);  // it has a copy now
-      else p.table_out[e] = __ldg(p.table_in + (int64_t)__ldg(p.source + i) * p.width + c);
-    } else if ((int64_t)c * P >= (int64_t)had + __ldg(p.add + i)) {
+      if (s_own[i] && c == had / P) atomicSub(holders.refs + s_last[i], 1);  // it has a copy now
+      else p.table_out[e] = __ldg(p.table_in + (int64_t)s_src[i] * p.width + c);
+    } else if ((int64_t)c * P >= (int64_t)had + s_add[i]) {
       p.table_out[e] = -1;
     }
+  });
+  for (int i = gt; i < n; i += all) {
+    p.kv_out[i] = s_had[i] + s_add[i];
+    if (!s_own[i]) *reinterpret_cast<int2*>(p.pairs + 2 * i) = make_int2(-1, -1);
   }
-  for (int i = gt; i < n; i += all) p.kv_out[i] = s_had[i] + __ldg(p.add + i);
   if (gt == 0) p.report[3] = n_free - need;
+  if constexpr (kOne) {
+    __syncthreads();
+    for (int i = tid; i < p.n_pages; i += kPagesThreads) p.refs[i] = holders.refs[i];
+  }
 }
 
+template <bool kOne>
 __global__ void __launch_bounds__(kPagesThreads) pages_compact_kernel(const __grid_constant__ PagesParams p) {
-  __shared__ int s_warp[32], s_live[kMaxPagesCluster], s_hole[kMaxPagesCluster], s_mover[kMaxPagesCluster];
-  const int n_cta = gridDim.x, rank = blockIdx.x, tid = threadIdx.x;
+  extern __shared__ int s_dyn[];
+  __shared__ int s_warp[32], s_live[kMaxPagesCluster], s_hole[kMaxPagesCluster], s_mover[kMaxPagesCluster], s_bad;
+  const Holders<kOne> holders{kOne ? s_dyn : p.refs};
+  const int n_cta = kOne ? 1 : gridDim.x, rank = kOne ? 0 : blockIdx.x, tid = threadIdx.x;
   const int gt = rank * kPagesThreads + tid, all = n_cta * kPagesThreads;
-  const int64_t entries = (int64_t)p.n_seqs * p.width;
   grid_go();
   grid_wait();
-  for (int i = gt; i < p.n_pages; i += all) p.refs[i] = 0;
+  if (tid == 0) s_bad = 0;
+  for (int i = gt; i < p.n_pages; i += all) holders.refs[i] = 0;
   if (gt < 4) p.report[gt] = 0;
-  cluster_sync();
-  auto kept = [&](int64_t e) {
-    const int i = (int)(e / p.width);
-    return (int)(e - (int64_t)i * p.width) < pages_of(__ldg(p.kv_in + i), p);
-  };
+  sync_all<kOne>();
+  int* const bad = kOne ? &s_bad : p.report + 2;
   for (int i = gt; i < p.n_seqs; i += all)
-    if (pages_of(__ldg(p.kv_in + i), p) < 0) atomicAdd(p.report + 2, 1);
-  for (int64_t e = gt; e < entries; e += all) {
-    if (!kept(e)) continue;
-    const int page = __ldg(p.table_in + e);
-    if ((unsigned)page < (unsigned)p.n_pages) atomicAdd(p.refs + page, 1);
-    else atomicAdd(p.report + 2, 1);
-  }
-  cluster_sync();
+    if (pages_of(__ldg(p.kv_in + i), p) < 0) atomicAdd(bad, 1);
+  for_entries(p.n_seqs, p.width, gt, all, [&](int i, int c, int64_t e) {
+    const int page = __ldg(p.table_in + e);  // (asked for before the length is known)
+    if (c >= pages_of(__ldg(p.kv_in + i), p)) return;
+    if ((unsigned)page < (unsigned)p.n_pages) atomicAdd(holders.refs + page, 1);
+    else atomicAdd(bad, 1);
+  });
+  sync_all<kOne>();
   const int chunk = (p.n_pages + n_cta - 1) / n_cta;
   const int first = min(p.n_pages, rank * chunk), end = min(p.n_pages, first + chunk);
-  auto live = [&](int page) { return __ldcg(p.refs + page) > 0; };
-  const int live_here = count_pages(first, end, s_warp, live);
-  if (tid == 0) tell_cluster(s_live, rank, n_cta, live_here);
-  cluster_sync();
-  int n_live = 0;
-  for (int r = 0; r < n_cta; ++r) n_live += s_live[r];
-  if (__ldcg(p.report + 2) > 0) {  // nothing is moved
-    for (int64_t e = gt; e < entries; e += all) p.table_out[e] = __ldg(p.table_in + e);
+  auto live = [&](int page) { return holders.get(page) > 0; };
+  int n_live = count_pages(first, end, s_warp, live);
+  if constexpr (!kOne) {
+    if (tid == 0) tell_cluster(s_live, rank, n_cta, n_live);
+    cluster_sync();
+    n_live = 0;
+    for (int r = 0; r < n_cta; ++r) n_live += s_live[r];
+  }
+  if ((kOne ? s_bad : __ldcg(p.report + 2)) > 0) {  // nothing is moved
+    for_entries(p.n_seqs, p.width, gt, all, [&](int, int, int64_t e) { p.table_out[e] = __ldg(p.table_in + e); });
     for (int i = gt; i < p.max_pairs; i += all) *reinterpret_cast<int2*>(p.pairs + 2 * i) = make_int2(-1, -1);
     if (gt == 0) {
       p.report[0] = n_live;
+      if (kOne) p.report[2] = s_bad;
       p.report[3] = p.n_pages - n_live;
     }
+    if constexpr (kOne)
+      for (int i = tid; i < p.n_pages; i += kPagesThreads) p.refs[i] = holders.refs[i];
     return;
   }
   // The holes are the free pages below n_live, the movers the live pages from there on: as many of the ones as of the others, and
   // no page is both, so the copies need no order.
   const int hole_end = min(end, max(first, n_live)), mover_first = max(first, min(end, n_live));
   auto hole = [&](int page) { return !live(page); };
-  const int holes_here = count_pages(first, hole_end, s_warp, hole), movers_here = count_pages(mover_first, end, s_warp, live);
-  if (tid == 0) {
-    tell_cluster(s_hole, rank, n_cta, holes_here);
-    tell_cluster(s_mover, rank, n_cta, movers_here);
-  }
-  cluster_sync();
-  int hole0 = 0, mover0 = 0, n_moves = 0;
-  for (int r = 0; r < n_cta; ++r) {
-    if (r < rank) {
-      hole0 += s_hole[r];
-      mover0 += s_mover[r];
+  int n_moves = count_pages(first, hole_end, s_warp, hole), hole0 = 0, mover0 = 0;
+  if constexpr (!kOne) {
+    const int movers_here = count_pages(mover_first, end, s_warp, live);
+    if (tid == 0) {
+      tell_cluster(s_hole, rank, n_cta, n_moves);
+      tell_cluster(s_mover, rank, n_cta, movers_here);
     }
-    n_moves += s_hole[r];
+    cluster_sync();
+    n_moves = 0;
+    for (int r = 0; r < n_cta; ++r) {
+      if (r < rank) {
+        hole0 += s_hole[r];
+        mover0 += s_mover[r];
+      }
+      n_moves += s_hole[r];
+    }
   }
   rank_pages(first, hole_end, hole0, s_warp, hole, [&](int page, int r) { p.pairs[2 * r + 1] = page; });
   rank_pages(mover_first, end, mover0, s_warp, live, [&](int page, int r) { p.pairs[2 * r] = page; });
   for (int i = n_moves + gt; i < p.max_pairs; i += all) *reinterpret_cast<int2*>(p.pairs + 2 * i) = make_int2(-1, -1);
-  cluster_sync();
+  sync_all<kOne>();
   // the holders go with the page; until the table is rewritten refs says where: -(target + 1)
-  rank_pages(mover_first, end, mover0, s_warp, live, [&](int page, int r) {
-    const int to = __ldcg(p.pairs + 2 * r + 1);
-    p.refs[to] = __ldcg(p.refs + page);
-    p.refs[page] = -to - 1;
-  });
-  cluster_sync();
-  for (int64_t e = gt; e < entries; e += all) {
-    int page = -1;
-    if (kept(e)) {
-      page = __ldg(p.table_in + e);
-      if (page >= n_live) page = -__ldcg(p.refs + page) - 1;
-    }
-    p.table_out[e] = page;
+  for (int r = gt; r < n_moves; r += all) {
+    const int2 e = __ldcg(reinterpret_cast<const int2*>(p.pairs + 2 * r));
+    holders.refs[e.y] = holders.get(e.x);
+    holders.refs[e.x] = -e.y - 1;
   }
-  cluster_sync();
-  for (int i = max(first, n_live) + tid; i < end; i += kPagesThreads) p.refs[i] = 0;
+  sync_all<kOne>();
+  for_entries(p.n_seqs, p.width, gt, all, [&](int i, int c, int64_t e) {
+    int page = __ldg(p.table_in + e);
+    if (c >= pages_of(__ldg(p.kv_in + i), p)) page = -1;
+    else if (page >= n_live) page = -holders.get(page) - 1;
+    p.table_out[e] = page;
+  });
   if (gt == 0) {
     p.report[0] = n_live;
     p.report[1] = n_moves;
     p.report[3] = p.n_pages - n_live;
+  }
+  sync_all<kOne>();
+  if constexpr (kOne) {
+    for (int i = tid; i < p.n_pages; i += kPagesThreads) p.refs[i] = i < n_live ? holders.refs[i] : 0;
+  } else {
+    for (int i = max(first, n_live) + tid; i < end; i += kPagesThreads) p.refs[i] = 0;
   }
 }
 
@@ -369,16 +419,23 @@ cudaError_t launch_pages_copy(const PagesCopyParams& p, cudaStream_t stream) {
   return launch_dependent(pages_copy_kernel, dim3((unsigned)std::min<int64_t>(pieces, 148 * 4)), kCopyThreads, 0, 1, true, stream, p);
 }
 
-static cudaError_t launch_pages(void (*kernel)(PagesParams), const PagesParams& p, size_t smem, cudaStream_t stream) {
-  cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeNonPortableClusterSizeAllowed, 1);
-  if (e == cudaSuccess && smem) e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
+// One CTA where the holders fit next to its tables and it has few entries to go through; a cluster otherwise.
+static bool one_cta(const PagesParams& p, size_t smem) { return smem + (size_t)p.n_pages * 4 <= 160 * 1024 && (int64_t)p.n_seqs * p.width <= 32768; }
+static cudaError_t launch_pages(void (*kernel)(PagesParams), const PagesParams& p, size_t smem, int n_cta, cudaStream_t stream) {
+  cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
+  if (e == cudaSuccess && n_cta > 8) e = cudaFuncSetAttribute(kernel, cudaFuncAttributeNonPortableClusterSizeAllowed, 1);
   if (e != cudaSuccess) return e;
-  return launch_dependent(kernel, dim3(kMaxPagesCluster), kPagesThreads, smem, kMaxPagesCluster, true, stream, p);
+  return launch_dependent(kernel, dim3(n_cta), kPagesThreads, smem, n_cta, true, stream, p);
 }
 cudaError_t launch_pages_fork(const PagesParams& p, cudaStream_t stream) {
   if (p.n_seqs > kMaxForkSeqs) return cudaErrorInvalidValue;
-  return launch_pages(pages_fork_kernel, p, (size_t)p.n_seqs * 12, stream);
+  const size_t smem = (size_t)p.n_seqs * 24;
+  if (one_cta(p, smem)) return launch_pages(pages_fork_kernel<true>, p, smem + (size_t)p.n_pages * 4, 1, stream);
+  return launch_pages(pages_fork_kernel<false>, p, smem, kMaxPagesCluster, stream);
 }
-cudaError_t launch_pages_compact(const PagesParams& p, cudaStream_t stream) { return launch_pages(pages_compact_kernel, p, 0, stream); }
+cudaError_t launch_pages_compact(const PagesParams& p, cudaStream_t stream) {
+  if (one_cta(p, 0)) return launch_pages(pages_compact_kernel<true>, p, (size_t)p.n_pages * 4, 1, stream);
+  return launch_pages(pages_compact_kernel<false>, p, 0, kMaxPagesCluster, stream);
+}
 
 }  // namespace cascade
