@@ -398,7 +398,9 @@ def cascade_rope_table_scaled(n_positions: int, rot_dim: int, base: float, kind:
     "linear", "base", "bands" or "ramp" (include/cascade.h has the formulas); attention 0: the kind's own factor on cos and sin."""
     if kind not in ROPE_KINDS:
         raise CascadeError(1, f"cascade_rope_table_scaled: unknown kind {kind!r}")
-    table = torch.empty((max(n_positions, 0), max(rot_dim, 0) // 2, 2), dtype=torch.float32, device=device)
+    table = None
+    if device != "cuda":  # (otherwise made by the call)
+        table = torch.empty((max(n_positions, 0), max(rot_dim, 0) // 2, 2), dtype=torch.float32, device=device)
     return _native().rope_table_scaled(n_positions, rot_dim, base, ROPE_KINDS[kind], factor, original_positions, low, high, attention, table)
 
 

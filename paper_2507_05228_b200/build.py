@@ -16,7 +16,7 @@ LIB = os.path.join(HERE, "libcascade_b200.so")
 FASTCALL = os.path.join(HERE, "_fastcall.so")
 LIB_DEBUG = os.path.join(HERE, "libcascade_b200_debug.so")
 SOURCES = ["cascade_api.cu", "merge.cu", "attn_simt.cu", "attn_rows.cu", "attn_tc.cu", "attn_split.cu", "gather.cu", "decode.cu", "decode_static.cu",
-           "shard_maps.cu", "rope.cu", "plan_advance.cu", "rope_rows.cu", "pages.cu", "paged_decode.cu", "paged_api.cu"]
+           "shard_maps.cu", "rope.cu", "plan_advance.cu", "rope_rows.cu", "pages.cu", "paged_decode.cu", "paged_f32.cu", "paged_api.cu"]
 NVCC_FLAGS = [
     "-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-O3", "-std=c++17",
     "-Xcompiler", "-fPIC", "-Xptxas", "-v", "-I", os.path.join(ROOT, "include"), "-I", CSRC,

@@ -15,10 +15,6 @@
 // plan before they are requested, and a shard of a few keys does not end in a chunk of its own.  (Shard by shard, one sequence of
 // 128 tokens had its key rows requested after 7000 of 14000 cycles.)
 //
-// kPaged (cascade_attn_paged): rows are (token, head) pairs of a sequence, the heads of a KV head side by side, and the keys the rows of
-// its pages; a chunk lies in one page.  Where rows are few, key_parts CTAs share the keys of a tile and leave partials, which
-// paged_combine_kernel adds up.
-//
 // RW = 4: the four warps own different rows and share the K/V tiles.  RW = 1: all four warps own the same rows and take the
 // tiles (32 keys) of the stream in turn; their (m, l, o) are combined at the end.  Small problems and short shards use the
 // latter: four times as many CTAs, four times shorter chains, less padding.
@@ -26,7 +22,7 @@
 // and merge 708 us, before 1662 us with one row at a time per warp); one sequence of 128 tokens, 12 heads, 2 shards: 8.4 us
 // (in token order; shard by shard 10.5, a row at a time 35).  What bounds it now is shared-memory bandwidth: 448 16-byte loads (4 cycles each) against 2048 packed FMAs
 // per warp and 16 x 64 tile.
-#include "paged.cuh"
+#include "cascade_internal.cuh"
 
 namespace cascade {
 
@@ -105,21 +101,18 @@ struct SimtCfg {
 constexpr int64_t kEnough = 2 * 148;  // CTAs that fill the chip, two per SM
 
 // A tile of the key stream: per chunk of 16 keys its first key in the stream and in the plan's list, and the keys from there on.
-template <int NC, bool kPaged>
+template <int NC>
 struct SimtTile {
-  int t0[NC], n[NC], at[NC];  // kPaged: at = row of the page
-  int page[kPaged ? NC : 1];
+  int t0[NC], n[NC], at[NC];
   bool any, masked;
 };
-enum SimtForm { kShards, kOfTokens, kOfPages };
 
-template <typename T, int D, int RW, int kForm>
+template <typename T, int D, int RW, bool kTokens>
 __global__ void __launch_bounds__(128, SimtCfg<D, RW>::kCtas)
-attn_simt_kernel(const __grid_constant__ AttnParams p, int parts_per_cta, int lg) {
+attn_simt_kernel(const __grid_constant__ AttnParams p, int parts_per_cta) {
   using C = SimtCfg<D, RW>;
   constexpr int TR = 4, NC = C::NC, BN = C::BN, KJ = BN / 8, DJ = D / 32;
   constexpr int kGroupThreads = RW * 32;
-  constexpr bool kPaged = kForm == kOfPages, kTokens = kForm != kShards;
   extern __shared__ __align__(16) float smem_f[];
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   const int group = warp / RW, gtid = tid % kGroupThreads;
@@ -135,27 +128,15 @@ attn_simt_kernel(const __grid_constant__ AttnParams p, int parts_per_cta, int lg
   const PlanDev& pl = p.plan;
   const int P = pl.n_kv_shards;
   const int n_pg = kTokens ? 1 : (P + parts_per_cta - 1) / parts_per_cta;
-  int b = kPaged ? 0 : kTokens ? blockIdx.z : blockIdx.z / n_pg;
+  const int b = kTokens ? blockIdx.z : blockIdx.z / n_pg;
   const int pg = kTokens ? 0 : blockIdx.z % n_pg;
-  const int key_part = kPaged ? blockIdx.z : 0;
-  const int map = kPaged || pl.n_maps == 1 ? 0 : b;
-  const int h = kPaged ? blockIdx.y << lg : blockIdx.y;  // kPaged: the first of the 1 << lg heads of the tile
+  const int map = pl.n_maps == 1 ? 0 : b;
+  const int h = blockIdx.y;
   const int g = p.G == 1 ? h : h / p.G;
   // the plan's tiles of 64 slots, or of 32 slots in two pieces
   constexpr int kList = RW == 4 ? 1 : 0, kPieces = (32 << kList) / C::R;
   int row0, nrows;  // slots of a query shard, or tokens, the last ones (which see most) first
-  int seq_row0 = 0, seq_rows = 0, seq_len = 0;  // kPaged: the rows and the length of the sequence
-  if constexpr (kPaged) {
-    const int2 t = paged_tile(p.paged, blockIdx.x, C::R >> lg, lane);
-    if (t.x < 0) return;
-    b = t.x;
-    const int2 rows = paged_rows(p.paged, b);
-    seq_row0 = rows.x;
-    seq_rows = rows.y;
-    seq_len = paged_len(p.paged, b);
-    row0 = t.y * (C::R >> lg);
-    nrows = min(C::R >> lg, seq_rows - row0) << lg;
-  } else if constexpr (kTokens) {
+  if constexpr (kTokens) {
     row0 = (int)(gridDim.x - 1 - blockIdx.x) * C::R;
     nrows = min(C::R, pl.n_q - row0);
   } else {
@@ -172,13 +153,10 @@ attn_simt_kernel(const __grid_constant__ AttnParams p, int parts_per_cta, int lg
   const int32_t* vis_first = vis + (size_t)row0 * P;
   const int32_t* vis_last = vis + (size_t)(row0 + nrows - 1) * P;
   auto token_of = [&](int r) {
-    if constexpr (kPaged) return (int64_t)(seq_row0 + row0 + (r >> lg));
-    else if constexpr (kTokens) return (int64_t)(row0 + r);
+    if constexpr (kTokens) return (int64_t)(row0 + r);
     else return (int64_t)CASCADE_CHECKED((int64_t)__ldg(q_idx + row0 + r), pl.n_q, pl.status, 104);
   };
-  auto head_of = [&](int r) { return kPaged ? h + (r & ((1 << lg) - 1)) : h; };
   auto seen_by = [&](int r) {  // kTokens: keys of the sequence that the row sees
-    if constexpr (kPaged) return paged_seen(p.paged, pl.causal, seq_rows, seq_len, row0 + (r >> lg), seq_row0 + row0 + (r >> lg));
     if (!pl.causal) return pl.n_kv;
     if (!p.prefix_from_vis) return (int)max((int64_t)0, min((int64_t)pl.n_kv, (int64_t)pl.q_pos_offset + row0 + r + 1));
     const int32_t* of = vis + (size_t)__ldg(pl.q_inv + (size_t)map * pl.n_q + row0 + r) * P;
@@ -186,25 +164,15 @@ attn_simt_kernel(const __grid_constant__ AttnParams p, int parts_per_cta, int lg
     for (int k = 0; k < P; ++k) n += __ldg(of + k);
     return n;
   };
-  int seen_first = kTokens ? seen_by(0) : 0, seen_last = kTokens ? seen_by(nrows - 1) : 0;
-  if constexpr (kPaged) {
-    if (p.paged.visible) {  // in any order
-      for (int r = 0; r < nrows; r += 1 << lg) {
-        const int n = seen_by(r);
-        seen_first = min(seen_first, n);
-        seen_last = max(seen_last, n);
-      }
-    }
-  }
-  const T* qb = static_cast<const T*>(p.q) + (kPaged ? 0 : (int64_t)b * p.qs.batch + (int64_t)h * p.qs.head);
-  const T* kb = static_cast<const T*>(p.k) + (kPaged ? 0 : (int64_t)b * p.ks.batch) + (int64_t)g * p.ks.head;
-  const T* vb = static_cast<const T*>(p.v) + (kPaged ? 0 : (int64_t)b * p.vs.batch) + (int64_t)g * p.vs.head;
+  const int seen_first = kTokens ? seen_by(0) : 0, seen_last = kTokens ? seen_by(nrows - 1) : 0;
+  const T* qb = static_cast<const T*>(p.q) + (int64_t)b * p.qs.batch + (int64_t)h * p.qs.head;
+  const T* kb = static_cast<const T*>(p.k) + (int64_t)b * p.ks.batch + (int64_t)g * p.ks.head;
+  const T* vb = static_cast<const T*>(p.v) + (int64_t)b * p.vs.batch + (int64_t)g * p.vs.head;
 
   for (int i = tid; i < C::R * (D / 4); i += 128) {
     const int r = i / (D / 4), c4 = (i % (D / 4)) * 4;
     const int64_t tok = r < nrows ? token_of(r) : (int64_t)0;
-    const int64_t head = kPaged && r < nrows ? (int64_t)head_of(r) * p.qs.head : 0;
-    stage4(sQ + r * C::QP + c4, qb + tok * p.qs.token + head + c4, r < nrows);
+    stage4(sQ + r * C::QP + c4, qb + tok * p.qs.token + c4, r < nrows);
   }
   stage_commit();
   auto group_sync = [&]() {
@@ -214,10 +182,9 @@ attn_simt_kernel(const __grid_constant__ AttnParams p, int parts_per_cta, int lg
   // one tile of K or V rows
   constexpr int kPerRow = D / 4, kRowsAtOnce = kGroupThreads / kPerRow;
   const int lr = gtid / kPerRow, lc = (gtid % kPerRow) * 4;
-  auto stage_tile = [&](const SimtTile<NC, kPaged>& t, const T* tensor, int64_t token_stride, int64_t page_stride, float* dst, int pitch) {
+  auto stage_tile = [&](const SimtTile<NC>& t, const T* base, int64_t token_stride, float* dst, int pitch) {
 #pragma unroll
-    for (int j = 0; j < NC; ++j) {
-      const T* base = kPaged ? tensor + t.page[kPaged ? j : 0] * page_stride : tensor;
+    for (int j = 0; j < NC; ++j)
 #pragma unroll
       for (int i = 0; i < 16 / kRowsAtOnce; ++i) {
         const int x = i * kRowsAtOnce + lr;
@@ -230,7 +197,6 @@ attn_simt_kernel(const __grid_constant__ AttnParams p, int parts_per_cta, int lg
         }
         stage4(dst + (j * 16 + x) * pitch + lc, base + tok * token_stride + lc, there);
       }
-    }
     stage_commit();
   };
   const int my_row = wrow + rg;  // this thread's rows: my_row + 4 r
@@ -255,15 +221,9 @@ attn_simt_kernel(const __grid_constant__ AttnParams p, int parts_per_cta, int lg
     }
     // cursor over the chunks of shard `part`, or of the sequence
     int c = group * NC;
-    int need = kTokens ? seen_last : __ldg(vis_last + part);
-    if constexpr (kPaged) {  // this CTA's part of the tiles of all groups
-      const int n_tiles = (need + 16 * NC * C::KW - 1) / (16 * NC * C::KW);
-      const int t0 = (int)((int64_t)n_tiles * key_part / p.key_parts), t1 = (int)((int64_t)n_tiles * (key_part + 1) / p.key_parts);
-      c += t0 * NC * C::KW;
-      need = min(need, t1 * 16 * NC * C::KW);
-    }
+    const int need = kTokens ? seen_last : __ldg(vis_last + part);
     const int first = kTokens ? seen_first : __ldg(vis_first + part), at0 = kTokens ? 0 : __ldg(kv_off + part);
-    auto next_tile = [&](SimtTile<NC, kPaged>& t) {
+    auto next_tile = [&](SimtTile<NC>& t) {
       t.masked = false;
       t.any = c * 16 < need;
 #pragma unroll
@@ -271,22 +231,17 @@ attn_simt_kernel(const __grid_constant__ AttnParams p, int parts_per_cta, int lg
         t.t0[j] = c * 16;
         t.n[j] = need - c * 16;
         t.at[j] = at0 + c * 16;
-        if constexpr (kPaged) {
-          const int index = c * 16 / p.paged.page_size;
-          t.page[j] = c * 16 < need ? paged_page(p.paged, b, index) : 0;
-          t.at[j] -= index * p.paged.page_size;
-        }
         t.masked = t.masked || first < c * 16 + 16;
         ++c;
       }
       c += (C::KW - 1) * NC;  // the other groups' tiles
     };
-    SimtTile<NC, kPaged> cur, nxt;
+    SimtTile<NC> cur, nxt;
     next_tile(cur);
     group_sync();  // the tiles of the previous part are consumed
     if (cur.any) {
-      stage_tile(cur, kb, p.ks.token, p.ks.batch, sK, C::KP);
-      stage_tile(cur, vb, p.vs.token, p.vs.batch, sV, D);
+      stage_tile(cur, kb, p.ks.token, sK, C::KP);
+      stage_tile(cur, vb, p.vs.token, sV, D);
     }
     // the query rows, staged by all threads, are the oldest group
     if (part == k_first) {
@@ -328,7 +283,7 @@ attn_simt_kernel(const __grid_constant__ AttnParams p, int parts_per_cta, int lg
       }
       next_tile(nxt);
       group_sync();  // K is consumed
-      if (nxt.any) stage_tile(nxt, kb, p.ks.token, p.ks.batch, sK, C::KP);
+      if (nxt.any) stage_tile(nxt, kb, p.ks.token, sK, C::KP);
       // mask, running maximum, weights
       if (cur.masked) {
 #pragma unroll
@@ -402,7 +357,7 @@ attn_simt_kernel(const __grid_constant__ AttnParams p, int parts_per_cta, int lg
         }
       }
       group_sync();  // V is consumed
-      if (nxt.any) stage_tile(nxt, vb, p.vs.token, p.vs.batch, sV, D);
+      if (nxt.any) stage_tile(nxt, vb, p.vs.token, sV, D);
       cur = nxt;
     }
 
@@ -413,20 +368,7 @@ attn_simt_kernel(const __grid_constant__ AttnParams p, int parts_per_cta, int lg
       o.y *= inv;
       o.z *= inv;
       o.w *= inv;
-      if constexpr (kPaged) {
-        const int64_t tok = token_of(row), head = head_of(row);
-        if (p.key_parts > 1) {
-          const int64_t stat = ((int64_t)key_part * p.paged.n_rows + tok) * p.H + head;
-          *reinterpret_cast<float4*>(static_cast<float*>(p.o_part) + stat * D + col) = o;
-          if (stats) {
-            p.m_part[stat] = l > 0.f ? m_raw * p.scale : -INFINITY;
-            p.l_part[stat] = l;
-          }
-        } else {
-          store4(static_cast<T*>(p.o_out) + tok * p.os.token + head * p.os.head + col, o);
-          if (stats && p.lse_out) p.lse_out[tok * p.H + head] = l > 0.f ? m_raw * p.scale + logf(l) : -INFINITY;
-        }
-      } else if constexpr (kTokens) {
+      if constexpr (kTokens) {
         const int64_t tok = row0 + row;
         store4(static_cast<T*>(p.o_out) + (int64_t)b * p.os.batch + tok * p.os.token + (int64_t)h * p.os.head + col,
                o);
@@ -491,14 +433,14 @@ attn_simt_kernel(const __grid_constant__ AttnParams p, int parts_per_cta, int lg
 template <typename T, int D, int RW>
 cudaError_t launch_rows(const AttnParams& p, int parts_per_cta, cudaStream_t stream) {
   using C = SimtCfg<D, RW>;
-  auto kernel = p.fused ? attn_simt_kernel<T, D, RW, kOfTokens> : attn_simt_kernel<T, D, RW, kShards>;
+  auto kernel = p.fused ? attn_simt_kernel<T, D, RW, true> : attn_simt_kernel<T, D, RW, false>;
   // per function and per device; cheap enough to repeat on every launch
   cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)C::kBytes);
   if (e != cudaSuccess) return e;
   constexpr int kList = RW == 4 ? 1 : 0, kPieces = (32 << kList) / C::R;
   const int n_pg = p.fused ? 1 : (p.plan.n_kv_shards + parts_per_cta - 1) / parts_per_cta;
   const dim3 grid(p.fused ? (p.plan.n_q + C::R - 1) / C::R : p.plan.n_qtiles[kList] * kPieces, p.H, p.batch * n_pg);
-  kernel<<<grid, 128, C::kBytes, stream>>>(p, parts_per_cta, 0);
+  kernel<<<grid, 128, C::kBytes, stream>>>(p, parts_per_cta);
   count_launch();
   return cudaGetLastError();
 }
@@ -565,98 +507,6 @@ cudaError_t launch_attn_simt(const AttnParams& p, cascade_dtype_t dtype, cudaStr
   }
   if (p.d == 128) return launch_one<float, 128>(p, stream);
   return launch_one<float, 64>(p, stream);
-}
-
-// ---------------------------------------------------------------------------------------------------- paged
-
-namespace {
-
-// o = sum over the parts of exp(m - n) l u / w for the rows that belong to a sequence; thread = four columns of a (row, head).
-template <typename T, int D>
-__global__ void __launch_bounds__(256) paged_combine_kernel(const __grid_constant__ AttnParams p) {
-  grid_go();
-  grid_wait();
-  const int64_t item = (int64_t)blockIdx.x * (256 / (D / 4)) + threadIdx.x / (D / 4);
-  const int col = threadIdx.x % (D / 4) * 4;
-  const int64_t all = (int64_t)p.paged.n_rows * p.H, row = item / p.H;
-  if (item >= all || row < __ldg(p.paged.row_start) || row >= __ldg(p.paged.row_start + p.paged.batch)) return;
-  float n = -INFINITY, w = 0.f;
-  float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
-  for (int k = 0; k < p.key_parts; ++k) n = fmaxf(n, __ldg(p.m_part + k * all + item));
-  for (int k = 0; k < p.key_parts; ++k) {
-    const float l = __ldg(p.l_part + k * all + item);
-    const float f = l > 0.f ? l * expf(__ldg(p.m_part + k * all + item) - n) : 0.f;
-    const float4 u = __ldg(reinterpret_cast<const float4*>(static_cast<const float*>(p.o_part) + (k * all + item) * D + col));
-    w += f;
-    o.x = fmaf(f, u.x, o.x);
-    o.y = fmaf(f, u.y, o.y);
-    o.z = fmaf(f, u.z, o.z);
-    o.w = fmaf(f, u.w, o.w);
-  }
-  const float inv = w > 0.f ? 1.f / w : 0.f;
-  const int head = (int)(item - row * p.H);
-  store4(static_cast<T*>(p.o_out) + row * p.os.token + head * p.os.head + col, make_float4(o.x * inv, o.y * inv, o.z * inv, o.w * inv));
-  if (col == 0 && p.lse_out) p.lse_out[item] = w > 0.f ? n + logf(w) : -INFINITY;
-}
-
-int paged_heads_log2(int G) {  // heads of a tile: as many of the G as a power of two divides, at most 8
-  int lg = 0;
-  while (lg < 3 && G % (2 << lg) == 0) ++lg;
-  return lg;
-}
-// Tiles of `height` (token, head) rows there may be: every sequence can end in one that is not full.
-int64_t paged_tiles(const AttnParams& p, int height) {
-  const int per = height >> paged_heads_log2(p.G);
-  return p.paged.batch == 1 ? (p.paged.n_rows + per - 1) / per : p.paged.n_rows / per + p.paged.batch;
-}
-// Sixty-four rows a CTA where that fills the chip, as use_wide()
-bool paged_wide(const AttnParams& p) {
-  const int lg = paged_heads_log2(p.G), per = 64 >> lg;
-  return ((int64_t)p.paged.n_rows / per) * (p.H >> lg) >= kEnough;
-}
-
-template <typename T, int D, int RW>
-cudaError_t launch_paged_rows(const AttnParams& p, cudaStream_t stream) {
-  using C = SimtCfg<D, RW>;
-  auto kernel = attn_simt_kernel<T, D, RW, kOfPages>;
-  cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)C::kBytes);
-  if (e != cudaSuccess) return e;
-  const int lg = paged_heads_log2(p.G);
-  kernel<<<dim3((unsigned)paged_tiles(p, C::R), p.H >> lg, p.key_parts), 128, C::kBytes, stream>>>(p, 1, lg);
-  count_launch();
-  return cudaGetLastError();
-}
-template <typename T, int D>
-cudaError_t launch_paged(const AttnParams& p, cudaStream_t stream) {
-  cudaError_t e = paged_wide(p) ? launch_paged_rows<T, D, 4>(p, stream) : launch_paged_rows<T, D, 1>(p, stream);
-  if (e != cudaSuccess || p.key_parts == 1) return e;
-  const int64_t items = (int64_t)p.paged.n_rows * p.H, per = 256 / (D / 4);
-  return launch_dependent(paged_combine_kernel<T, D>, dim3((unsigned)((items + per - 1) / per)), 256, 0, 1, true, stream, p);
-}
-
-}  // namespace
-
-// Two CTAs per SM, each with at least 512 keys of what the table can hold.
-int paged_alu_parts(const AttnParams& p) {
-  if (paged_wide(p)) return 1;
-  const int64_t ctas = paged_tiles(p, 16) * (p.H >> paged_heads_log2(p.G)), keys = (int64_t)p.paged.max_pages * p.paged.page_size;
-  return (int)std::max<int64_t>(1, std::min<int64_t>({kEnough / std::max<int64_t>(1, ctas), keys / 512, 64}));
-}
-size_t paged_alu_ws_bytes(const AttnParams& p) {
-  const int64_t parts = paged_alu_parts(p);
-  return parts == 1 ? 0 : (size_t)(parts * p.paged.n_rows * p.H * (p.d + 2) * 4 + 512);
-}
-cudaError_t launch_paged_alu(AttnParams p, cascade_dtype_t dtype, void* workspace, cudaStream_t stream) {
-  p.key_parts = paged_alu_parts(p);
-  if (p.key_parts > 1) {
-    const int64_t items = (int64_t)p.key_parts * p.paged.n_rows * p.H;
-    p.o_part = workspace;
-    p.m_part = static_cast<float*>(workspace) + items * p.d;
-    p.l_part = p.m_part + items;
-  }
-  TimedLaunch timed(stream);
-  if (dtype == CASCADE_BF16) return p.d == 128 ? launch_paged<__nv_bfloat16, 128>(p, stream) : launch_paged<__nv_bfloat16, 64>(p, stream);
-  return p.d == 128 ? launch_paged<float, 128>(p, stream) : launch_paged<float, 64>(p, stream);
 }
 
 }  // namespace cascade

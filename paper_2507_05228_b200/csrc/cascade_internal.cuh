@@ -80,7 +80,7 @@ struct AttnParams {
   // Paged calls: K and V are pages (ks.batch, vs.batch: from page to page; token: from row to row of a page), q and o_out rows of
   // all sequences one after another.  Of `plan` only causal and status are set.
   PagedDev paged;
-  int32_t key_parts;  // paged ALU kernel: CTAs that share the keys of a tile; more than one: partials [key_parts][n_rows][H]
+  int32_t key_parts;  // paged fp32 kernel: CTAs that share the keys of a tile; more than one: partials [key_parts][n_rows][H]
   int32_t alone;      // paged decode kernel: no other kernel takes what it does not
 };
 
@@ -294,10 +294,9 @@ cudaError_t launch_merge_peers(const MergePeersParams& p, cascade_dtype_t dtype,
 // ---- paged caches
 // The device words that paged calls report to, of the current device (part of the module, nothing is allocated); null on error.
 int32_t* paged_status_words();
-// fp32, and bf16 where nothing else takes it: CTAs that share the keys of a tile, bytes of the partials they leave, the launch
-int paged_alu_parts(const AttnParams& p);
-size_t paged_alu_ws_bytes(const AttnParams& p);
-cudaError_t launch_paged_alu(AttnParams p, cascade_dtype_t dtype, void* workspace, cudaStream_t stream);
+// fp32: bytes of the partials that CTAs leave which share the keys of a tile, the launch
+size_t paged_f32_ws_bytes(const AttnParams& p);
+cudaError_t launch_paged_f32(AttnParams p, void* workspace, cudaStream_t stream);
 // bf16 on the tensor cores, where a tensor map holds the pages
 bool paged_tc_takes(const AttnParams& p);
 // bf16, sequences of at most paged_decode_rows() rows: heads of an item, scratch for sequences of at most `rows` rows, the launch

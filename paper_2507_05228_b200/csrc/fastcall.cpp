@@ -394,18 +394,19 @@ double real(PyObject* o) {
   if (v == -1.0 && PyErr_Occurred()) throw PyFailure();
   return v;
 }
-// (n_positions, rot_dim, base, kind, factor, original_positions, low, high, attention, table) -> table
+// (n_positions, rot_dim, base, kind, factor, original_positions, low, high, attention, table or None: on the current device) -> table
 PyObject* rope_table_scaled(PyObject* const* a) {
   const long long n = integer(a[0]), rot = integer(a[1]);
   need(n > INT32_MIN && n <= INT32_MAX && rot > INT32_MIN && rot <= INT32_MAX, "n_positions and rot_dim are 32-bit numbers");
   const int32_t kind = (int32_t)integer(a[3]);
   const double base = real(a[2]), factor = real(a[4]), original = real(a[5]), low = real(a[6]), high = real(a[7]), attention = real(a[8]);
-  const at::Tensor& table = here(a[9]);
+  const at::Tensor table = a[9] != Py_None ? here(a[9])
+                                           : at::empty({std::max(n, 0LL), std::max(rot, 0LL) / 2, 2},
+                                                       at::TensorOptions(at::kFloat).device(at::kCUDA, c10::cuda::current_device()));
   auto* tp = static_cast<float*>(table.data_ptr());
   void* st = stream();
   check(unlocked([&] { return api.rope_table_scaled((int32_t)n, (int32_t)rot, base, kind, factor, original, low, high, attention, tp, st); }));
-  Py_INCREF(a[9]);
-  return a[9];
+  return wrap(table);
 }
 
 // (x, positions, rope_table, interleaved, out or None) -> out

@@ -278,7 +278,7 @@ AttnParams paged_shape(int32_t batch, int32_t n_rows, int32_t max_rows, int32_t 
   return p;
 }
 // Which kernels take the sequences of a bf16 call: those of at most `rows` rows the decode kernel (0: none), the others the tensor-core
-// kernel on tiles.  (The ALU kernel takes all where no tensor map holds the pages.)
+// kernel on tiles.
 struct PagedRoute {
   int rows;
   bool tiles;
@@ -288,11 +288,10 @@ PagedRoute paged_route(const AttnParams& p, int32_t max_rows) {
   if (std::min(max_rows, p.paged.n_rows) <= few) return {std::min(max_rows, p.paged.n_rows), false};
   return {p.paged.batch == 1 ? 0 : few, true};  // (one sequence: its rows are max_rows, unless they are padded)
 }
-size_t align256(size_t n) { return (n + 255) / 256 * 256; }
 size_t paged_ws_bytes(const AttnParams& p, cascade_dtype_t dtype, int32_t max_rows) {
-  if (dtype == CASCADE_F32) return paged_alu_ws_bytes(p);
+  if (dtype == CASCADE_F32) return paged_f32_ws_bytes(p);
   const PagedRoute r = paged_route(p, max_rows);
-  return std::max(r.rows > 0 ? align256(paged_decode_ws_bytes(p, r.rows)) : 0, r.tiles ? paged_alu_ws_bytes(p) : 0);
+  return r.rows > 0 ? paged_decode_ws_bytes(p, r.rows) : 0;
 }
 
 }  // namespace
@@ -358,9 +357,9 @@ cascade_status_t cascade_attn_paged(cascade_dtype_t dtype, int32_t batch, int32_
   p.os = {0, o_strides.token, o_strides.head};
   p.lse_out = lse_out;
   cudaStream_t st = (cudaStream_t)stream;
-  if (dtype == CASCADE_F32) return launched(launch_paged_alu(p, dtype, workspace, st), fn);
+  if (dtype == CASCADE_F32) return launched(launch_paged_f32(p, workspace, st), fn);
   const PagedRoute r = paged_route(p, max_rows);
-  if (r.tiles && !paged_tc_takes(p)) return launched(launch_paged_alu(p, dtype, workspace, st), fn);
+  if (!paged_tc_takes(p)) return fail(CASCADE_ERR_UNSUPPORTED, fn, "bf16 pages whose strides are not positive and below 2^38 elements");
   cudaError_t e = cudaSuccess;
   if (r.tiles) {
     AttnParams many = p;

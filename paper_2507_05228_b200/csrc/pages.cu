@@ -363,7 +363,7 @@ __global__ void __launch_bounds__(kPagesThreads) pages_compact_kernel(const __gr
 
 // Every CTA lists the valid pairs, 2048 at a time, and takes its share of their pages piece by piece: most of the list may be empty
 // (fork: a pair a sequence; compaction: half the pool).
-constexpr int kCopyThreads = 512, kCopyWindow = 2048, kCopyLoads = 4, kCopyPiece = kCopyThreads * 16 * kCopyLoads;
+constexpr int kCopyThreads = 512, kCopyWindow = 2048, kCopyLoads = 8, kCopyPiece = kCopyThreads * 16 * kCopyLoads;
 
 __global__ void __launch_bounds__(kCopyThreads) pages_copy_kernel(const __grid_constant__ PagesCopyParams p) {
   __shared__ int2 s_pair[kCopyWindow];
@@ -416,7 +416,7 @@ __global__ void __launch_bounds__(kCopyThreads) pages_copy_kernel(const __grid_c
 
 cudaError_t launch_pages_copy(const PagesCopyParams& p, cudaStream_t stream) {
   const int64_t pieces = (int64_t)p.n_pairs * p.n_pools * ((p.page_bytes + kCopyPiece - 1) / kCopyPiece);
-  return launch_dependent(pages_copy_kernel, dim3((unsigned)std::min<int64_t>(pieces, 148 * 4)), kCopyThreads, 0, 1, true, stream, p);
+  return launch_dependent(pages_copy_kernel, dim3((unsigned)std::min<int64_t>(pieces, 148 * 2)), kCopyThreads, 0, 1, true, stream, p);
 }
 
 // One CTA where the holders fit next to its tables and it has few entries to go through; a cluster otherwise.
