@@ -32,17 +32,17 @@ __device__ __forceinline__ uint32_t pack2_bf16(float lo, float hi) {
 }
 
 // 32 bytes, streaming; volatile so that the loads stay where the pipeline below puts them
-__device__ __forceinline__ void load32(const __nv_bfloat16* p, uint32_t* r) {
+__device__ __forceinline__ void load32(const void* p, uint32_t* r) {
 #pragma unroll
   for (int i = 0; i < 8; i += 4)
     asm volatile("ld.global.cs.v4.b32 {%0, %1, %2, %3}, [%4];"
                  : "=r"(r[i]), "=r"(r[i + 1]), "=r"(r[i + 2]), "=r"(r[i + 3])
-                 : "l"(p + 2 * i)
+                 : "l"(static_cast<const char*>(p) + 4 * i)
                  : "memory");
 }
 
 // 16 bytes, the same way
-__device__ __forceinline__ void load16(const __nv_bfloat16* p, uint32_t* r) {
+__device__ __forceinline__ void load16(const void* p, uint32_t* r) {
   asm volatile("ld.global.cs.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "l"(p) : "memory");
 }
 

@@ -277,21 +277,21 @@ AttnParams paged_shape(int32_t batch, int32_t n_rows, int32_t max_rows, int32_t 
   p.paged.most = max_rows;
   return p;
 }
-// Which kernels take the sequences of a bf16 call: those of at most `rows` rows the decode kernel (0: none), the others the tensor-core
-// kernel on tiles.
+// Which kernels take the sequences of a call: those of at most `rows` rows the decode kernel (0: none), the others a kernel on tiles.
 struct PagedRoute {
   int rows;
   bool tiles;
 };
-PagedRoute paged_route(const AttnParams& p, int32_t max_rows) {
+PagedRoute paged_route(const AttnParams& p, cascade_dtype_t dtype, int32_t max_rows) {
   const int few = paged_decode_rows(p);
   if (std::min(max_rows, p.paged.n_rows) <= few) return {std::min(max_rows, p.paged.n_rows), false};
-  return {p.paged.batch == 1 ? 0 : few, true};  // (one sequence: its rows are max_rows, unless they are padded)
+  // One sequence has max_rows rows, unless they are padded.  In fp32 the kernel on tiles takes all: what adds up the parts of its keys
+  // writes every row.
+  return {p.paged.batch == 1 || dtype == CASCADE_F32 ? 0 : few, true};
 }
 size_t paged_ws_bytes(const AttnParams& p, cascade_dtype_t dtype, int32_t max_rows) {
-  if (dtype == CASCADE_F32) return paged_f32_ws_bytes(p);
-  const PagedRoute r = paged_route(p, max_rows);
-  return r.rows > 0 ? paged_decode_ws_bytes(p, r.rows) : 0;
+  const PagedRoute r = paged_route(p, dtype, max_rows);
+  return r.rows > 0 ? paged_decode_ws_bytes(p, dtype, r.rows) : dtype == CASCADE_F32 ? paged_f32_ws_bytes(p) : 0;
 }
 
 }  // namespace
@@ -357,19 +357,19 @@ cascade_status_t cascade_attn_paged(cascade_dtype_t dtype, int32_t batch, int32_
   p.os = {0, o_strides.token, o_strides.head};
   p.lse_out = lse_out;
   cudaStream_t st = (cudaStream_t)stream;
-  if (dtype == CASCADE_F32) return launched(launch_paged_f32(p, workspace, st), fn);
-  const PagedRoute r = paged_route(p, max_rows);
-  if (!paged_tc_takes(p)) return fail(CASCADE_ERR_UNSUPPORTED, fn, "bf16 pages whose strides are not positive and below 2^38 elements");
+  if (dtype == CASCADE_BF16 && !paged_tc_takes(p))
+    return fail(CASCADE_ERR_UNSUPPORTED, fn, "bf16 pages whose strides are not positive and below 2^38 elements");
+  const PagedRoute r = paged_route(p, dtype, max_rows);
   cudaError_t e = cudaSuccess;
   if (r.tiles) {
     AttnParams many = p;
     many.paged.least = r.rows + 1;
-    e = launch_paged_tc(many, st);
+    e = dtype == CASCADE_BF16 ? launch_paged_tc(many, st) : launch_paged_f32(many, workspace, st);
   }
   if (e == cudaSuccess && r.rows > 0) {
     p.paged.most = r.rows;
     p.alone = !r.tiles;
-    e = launch_paged_decode(p, r.rows, workspace, st);
+    e = launch_paged_decode(p, dtype, r.rows, workspace, st);
   }
   return launched(e, fn);
 }

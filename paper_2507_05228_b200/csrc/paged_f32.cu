@@ -1,5 +1,5 @@
-// fp32 attention over a paged cache (cascade_attn_paged): warp-level tensor-core products m16n8k8 on operands taken apart into two tf32
-// parts, x = hi + lo with hi the upper 11 bits of the mantissa: hi hi + hi lo + lo hi keeps what lies above 2^-21 of a product.
+// fp32 attention over a paged cache (cascade_attn_paged, sequences of more rows than paged_decode.cu takes): warp-level tensor-core
+// products m16n8k8 on operands taken apart into two tf32 parts (tf32.cuh).
 // (On the packed fp32 ALUs 8 sequences of 17 to 128 rows over 60 to 512 keys, 12 heads of 64, took 44 us, so 29.)
 //
 // The tensor core adds with truncation, so its sums are kept short: the logits over head_dim, the outputs over 32 keys, the small
@@ -21,6 +21,7 @@
 #include <algorithm>
 
 #include "paged.cuh"
+#include "tf32.cuh"
 
 namespace cascade {
 
@@ -35,23 +36,6 @@ __device__ __forceinline__ float ex2(float x) {
   asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
   return y;
 }
-__device__ __forceinline__ void mma_tf32(float (&c)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
-  asm volatile(
-      "mma.sync.aligned.m16n8k8.row.col.f32.tf32.tf32.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
-      : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
-      : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
-}
-// x = hi + lo, lo rounded to tf32 by the product's truncation.  hi is cut off for keys and values, and rounded for queries and
-// weights: the signs of the parts that hi leaves out are then not those of the operands on both sides, and the missing lo lo averages out.
-__device__ __forceinline__ void cut(float x, uint32_t& hi, uint32_t& lo) {
-  hi = __float_as_uint(x) & 0xffffe000u;
-  lo = __float_as_uint(x - __uint_as_float(hi)) + 0x1000u;
-}
-__device__ __forceinline__ void cut_rounded(float x, uint32_t& hi, uint32_t& lo) {
-  hi = (__float_as_uint(x) + 0x1000u) & 0xffffe000u;
-  lo = __float_as_uint(x - __uint_as_float(hi)) + 0x1000u;
-}
-
 constexpr int kTile = 32, NK = kTile / 8;  // keys of a tile, products side by side
 
 template <int D, int MT, int RW, int KW>

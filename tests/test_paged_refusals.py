@@ -101,11 +101,11 @@ def test_attention(L):
     refuses(f, args, 1, b"aligned", _12=cb.Strides(16 * 512, 512, 132))
     refuses(f, args, 3, _1=65536)
     n = ctypes.c_size_t()
-    sizes = [0, 1, 2, 2, 8, 2, 64, 16, 4096]
+    sizes = [0, 1, 32, 32, 8, 2, 64, 16, 4096]
     assert L.cascade_attn_paged_workspace_bytes(*sizes, ctypes.byref(n)) == 0 and n.value > 0
-    refuses(f, args, 4, b"workspace", _0=0, _1=1, _2=2, _3=2, _4=8, _5=2, _6=64, _18=4096, _19=4096, _27=n.value - 1)
-    refuses(f, args, 4, b"workspace", _0=0, _1=1, _2=2, _3=2, _4=8, _5=2, _6=64, _18=4096, _19=4096, _26=None)
-    refuses(f, args, 4, b"workspace", _0=0, _1=1, _2=2, _3=2, _4=8, _5=2, _6=64, _18=4096, _19=4096, _26=P + 16)
+    refuses(f, args, 4, b"workspace", _0=0, _1=1, _2=32, _3=32, _4=8, _5=2, _6=64, _18=4096, _19=4096, _27=n.value - 1)
+    refuses(f, args, 4, b"workspace", _0=0, _1=1, _2=32, _3=32, _4=8, _5=2, _6=64, _18=4096, _19=4096, _26=None)
+    refuses(f, args, 4, b"workspace", _0=0, _1=1, _2=32, _3=32, _4=8, _5=2, _6=64, _18=4096, _19=4096, _26=P + 16)
     for place in range(1, 9):
         bad = list(sizes)
         bad[place] = 0
