@@ -10,14 +10,17 @@
 // fp32 the same way with m16n8k8 products of operands cut into two tf32 parts (tf32.cuh); weights go from the lanes of their keys to
 // those of their columns by shuffles, and every block's products with the values are summed by themselves and added in fp32.
 //
-// How the keys are shared out.
-//   Few (sequence, KV head) items: a cluster of CTAs has one and adds up in distributed shared memory; one launch.
-//   Many: lengths differ between sequences, so the 16-key blocks of all items, one after another, are cut into as many equal ranges as
-//   CTAs are resident; an item that a range covers whole is finished there, one that is cut leaves partials, which a second, small
-//   kernel adds up (a CTA for each place where an item is first cut).  Where the ranges start follows from the lengths, which only
-//   the device knows: every CTA adds the blocks up for itself.
+// How the keys are shared out (rules and times at cluster_size).  Lengths differ between sequences, and only the device knows them.
+//   Few (sequence, KV head) items over short caches, or one sequence: a cluster of CTAs has one and adds up in distributed shared
+//   memory; one launch.
+//   Few otherwise: every item gets a CTA, and the other CTAs of the chip go to the items by their length; what the CTAs of an item
+//   leave is added up by a second, small kernel.
+//   Many: the 16-key blocks of all items, one after another, are cut into as many equal ranges as CTAs are resident; an item that a
+//   range covers whole is finished there, one that is cut leaves partials for the second kernel.
+// Who has what follows from the lengths, which every CTA adds up for itself.
 #include <algorithm>
 #include <type_traits>
+#include <utility>
 
 #include "decode_common.cuh"
 #include "paged.cuh"
@@ -27,7 +30,7 @@ namespace cascade {
 
 namespace {
 
-constexpr int kWarps = 8, kThreads = kWarps * 32;
+constexpr int kWarps = 8, kThreads = kWarps * 32, kJoinThreads = 128;
 constexpr int kMaxGroups = 2048;  // groups of 32 sequences
 constexpr int kClusterMost = 16;
 
@@ -40,7 +43,8 @@ struct RangeStart {
 struct DecodeArgs {
   int32_t Gi, items;  // heads of an item, items of a sequence
   int32_t n_cta;      // CTAs of the grid (ranges), or of a cluster
-  RangeStart* starts;  // [n_cta]
+  RangeStart* starts;  // [n_cta], ranges
+  int4* joins;         // [n_cta], shares: of the item whose first part is the CTA's, see paged_decode_join_shares_kernel
   float* partials;     // [n_cta][2][columns][D + 2]: of an item that starts before the range, and of one that ends behind it
 };
 
@@ -484,9 +488,144 @@ __global__ void __launch_bounds__(kThreads, 1) paged_decode_cluster_kernel(const
   end(p);
 }
 
+// Zeros for the rows over an empty cache, by one warp of CTA `cta`
+template <typename T, int D>
+__device__ __forceinline__ void clear_empty(const AttnParams& p, int cta, int n_cta, int lane) {
+  for (int b = cta + n_cta * lane; b < p.paged.batch; b += 32 * n_cta) {
+    const int2 rows = paged_rows(p.paged, b);
+    if (rows.y < p.paged.least || rows.y > p.paged.most || paged_len(p.paged, b) > 0) continue;
+    for (int64_t e = 0; e < (int64_t)rows.y * p.H; ++e) {
+      const int64_t row = rows.x + e / p.H, head = e % p.H;
+      uint4* o = reinterpret_cast<uint4*>(static_cast<T*>(p.o_out) + row * p.os.token + head * p.os.head);
+      for (int c = 0; c < D * (int)sizeof(T) / 16; ++c) o[c] = make_uint4(0u, 0u, 0u, 0u);
+      if (p.lse_out) p.lse_out[row * p.H + head] = -INFINITY;
+    }
+  }
+}
+
+// ---- a share of one item per CTA
+// Every item that has blocks gets a CTA, and what is left of them goes to the items by their length.
+constexpr int kSets = 3;  // of 32 sequences
+struct Share {
+  int b, item, row0, rows, len;  // b -1: none
+  int part, parts;
+};
+__device__ __forceinline__ Share share_of(const AttnParams& p, const DecodeArgs& a, int cta, int lane) {
+  const PagedDev& g = p.paged;
+  int row0[kSets], rows[kSets], len[kSets], total = 0, filled = 0;
+#pragma unroll
+  for (int s = 0; s < kSets; ++s) {
+    row0[s] = rows[s] = len[s] = 0;
+    const int b = 32 * s + lane;
+    if (b < g.batch) {
+      const int2 r = paged_rows(g, b);
+      row0[s] = r.x;
+      rows[s] = r.y;
+      len[s] = paged_len(g, b);
+      if (r.y > g.most && p.alone && cta == 0) paged_report(g.status, kBadRows, b, r.y);
+      if (r.y < g.least || r.y > g.most) rows[s] = len[s] = 0;
+    }
+    total += (len[s] + 15) / 16;
+    filled += len[s] > 0;
+  }
+  total = __reduce_add_sync(0xffffffffu, total);
+  filled = __reduce_add_sync(0xffffffffu, filled) * a.items;
+  const int spare = max(0, a.n_cta - filled);
+  Share r = {-1, 0, 0, 0, 0, 0, 1};
+  int before = 0;
+#pragma unroll
+  for (int s = 0; s < kSets; ++s) {
+    const int nb = (len[s] + 15) / 16;
+    const int n = nb ? min((nb + kWarps - 1) / kWarps, 1 + (int)((int64_t)nb * spare / ((int64_t)total * a.items))) : 0;
+    int incl = n * a.items;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+      const int t = __shfl_up_sync(0xffffffffu, incl, o);
+      if (lane >= o) incl += t;
+    }
+    const int off = cta - (before + incl - n * a.items);
+    const uint32_t mine = __ballot_sync(0xffffffffu, off >= 0 && off < n * a.items);
+    if (mine) {
+      const int who = __ffs(mine) - 1, at = __shfl_sync(0xffffffffu, off, who);
+      r.b = 32 * s + who;
+      r.row0 = __shfl_sync(0xffffffffu, row0[s], who);
+      r.rows = __shfl_sync(0xffffffffu, rows[s], who);
+      r.len = __shfl_sync(0xffffffffu, len[s], who);
+      r.parts = __shfl_sync(0xffffffffu, n, who);
+      r.part = at / a.items;  // the KV heads of the same keys side by side
+      r.item = at - r.part * a.items;
+    }
+    before += __shfl_sync(0xffffffffu, incl, 31);
+  }
+  return r;
+}
+
+template <typename T, int D, int NT, int kAhead>
+__global__ void __launch_bounds__(kThreads, 1) paged_decode_shares_kernel(const __grid_constant__ AttnParams p, const __grid_constant__ DecodeArgs a) {
+  extern __shared__ __align__(16) uint8_t smem[];
+  Shared<T, D, NT>& sh = *reinterpret_cast<Shared<T, D, NT>*>(smem);
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, cta = blockIdx.x;
+  begin(p);
+  if (warp == kWarps - 1) clear_empty<T, D>(p, cta, a.n_cta, lane);
+  const Share r = share_of(p, a, cta, lane);
+  if (tid == 0) a.joins[cta] = make_int4(r.b < 0 || r.part > 0 || r.parts == 1 ? 0 : r.parts, r.row0, r.rows, r.item);
+  if (r.b < 0) {
+    end(p);
+    return;
+  }
+  load_queries(sh, p, a, r.row0, r.rows, r.item, warp, lane);
+  const Walk<T, D, NT> walk = make_walk<T, D, NT>(p, a, r.b, r.row0, r.rows, r.len, r.item, lane);
+  State<D, NT> st;
+  clear(st);
+  const int blocks = (r.len + 15) / 16, last = (int)((int64_t)blocks * (r.part + 1) / r.parts), first = (int)((int64_t)blocks * r.part / r.parts) + warp;
+  walk.template run<kAhead>(st, sh.q, first, kWarps, first < last ? (last - first + kWarps - 1) / kWarps : 0, []() { __syncthreads(); });
+  publish(sh, st, warp, lane);
+  __syncthreads();
+  float* part = a.partials + (int64_t)cta * (8 * NT * (D + 2));
+  for (int i = tid; i < r.rows * a.Gi * D; i += kThreads) {
+    const int col = i / D, c = i % D;
+    float n, w, acc;
+    combine_warps(sh, col, c, n, w, acc);
+    if (r.parts == 1) {
+      write_out<T>(p, a, r.row0, r.item, col, c, n, w, acc);
+    } else {
+      part[i] = acc;
+      if (c == 0) {
+        part[8 * NT * D + col] = n;
+        part[8 * NT * (D + 1) + col] = w;
+      }
+    }
+  }
+  end(p);
+}
+
+// CTA (i, y) adds up a share of the columns of the item of which CTA i had the first part.
+template <typename T, int D, int NT>
+__global__ void __launch_bounds__(kJoinThreads) paged_decode_join_shares_kernel(const __grid_constant__ AttnParams p, const __grid_constant__ DecodeArgs a) {
+  grid_go();
+  grid_wait();
+  const int4 j = __ldcg(a.joins + blockIdx.x);  // parts (0: none), first row, rows, item
+  const int i = blockIdx.y * kJoinThreads + threadIdx.x;
+  if (i >= j.z * a.Gi * D || j.x == 0) return;
+  const int col = i / D, c = i % D;
+  auto part = [&](int k) { return a.partials + (int64_t)(blockIdx.x + k * a.items) * (8 * NT * (D + 2)); };
+  float n = -INFINITY, w = 0.f, acc = 0.f;
+#pragma unroll 4
+  for (int k = 0; k < j.x; ++k) n = fmaxf(n, __ldcg(part(k) + 8 * NT * D + col));
+  const float n_use = n == -INFINITY ? 0.f : n;
+#pragma unroll 4
+  for (int k = 0; k < j.x; ++k) {
+    const float* q = part(k);
+    const float f = ex2f(__ldcg(q + 8 * NT * D + col) - n_use);
+    w = fmaf(f, __ldcg(q + 8 * NT * (D + 1) + col), w);
+    acc = fmaf(f, __ldcg(q + i), acc);
+  }
+  write_out<T>(p, a, j.y, j.w, col, c, n, w, acc);
+}
+
 // ---- ranges of equal length
 template <typename T, int D, int NT, int kAhead>
-__global__ void __launch_bounds__(kThreads, sizeof(T) == 2 ? 3 - kAhead : 1) paged_decode_ranges_kernel(const __grid_constant__ AttnParams p, const __grid_constant__ DecodeArgs a) {
+__global__ void __launch_bounds__(kThreads, sizeof(T) == 2 && D == 64 ? 2 : 1) paged_decode_ranges_kernel(const __grid_constant__ AttnParams p, const __grid_constant__ DecodeArgs a) {
   extern __shared__ __align__(16) uint8_t smem[];
   Shared<T, D, NT>& sh = *reinterpret_cast<Shared<T, D, NT>*>(smem);
   __shared__ int s_group[kMaxGroups + 1];  // blocks (of one item) of the groups of 32 sequences before
@@ -494,6 +633,7 @@ __global__ void __launch_bounds__(kThreads, sizeof(T) == 2 ? 3 - kAhead : 1) pag
   const PagedDev& g = p.paged;
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, cta = blockIdx.x;
   begin(p);
+  if (warp == kWarps - 1) clear_empty<T, D>(p, cta, a.n_cta, lane);
   const int groups = (g.batch + 31) / 32;
   for (int i = warp; i < groups; i += kWarps) {
     const int b = i * 32 + lane, n = b < g.batch ? blocks_of(g, b) : 0;
@@ -502,17 +642,6 @@ __global__ void __launch_bounds__(kThreads, sizeof(T) == 2 ? 3 - kAhead : 1) pag
     if (cta == 0 && b < g.batch) {
       const int rows = paged_rows(g, b).y;
       if (rows > g.most && p.alone) paged_report(g.status, kBadRows, b, rows);  // nobody else takes it
-    }
-    // rows over an empty cache
-    if (b < g.batch && n == 0 && b % a.n_cta == cta) {
-      const int2 rows = paged_rows(g, b);
-      if (rows.y >= g.least && rows.y <= g.most)
-        for (int64_t e = 0; e < (int64_t)rows.y * p.H; ++e) {
-          const int64_t row = rows.x + e / p.H, head = e % p.H;
-          uint4* o = reinterpret_cast<uint4*>(static_cast<T*>(p.o_out) + row * p.os.token + head * p.os.head);
-          for (int c = 0; c < D * (int)sizeof(T) / 16; ++c) o[c] = make_uint4(0u, 0u, 0u, 0u);
-          if (p.lse_out) p.lse_out[row * p.H + head] = -INFINITY;
-        }
     }
   }
   __syncthreads();
@@ -659,13 +788,20 @@ cudaError_t with_shape(cascade_dtype_t dtype, int d, int columns, F f) {
 
 int ranges_cta(cascade_dtype_t dtype, int d) { return d == 128 || dtype == CASCADE_F32 ? 148 : 296; }  // CTAs that are resident at a time
 int64_t decode_items(const AttnParams& p) { return (int64_t)p.paged.batch * (p.H / paged_decode_heads(p)); }
-int cluster_size(const AttnParams& p) {  // 0: ranges
-  const int64_t items = decode_items(p);
-  if (items > 32) return 0;
-  const int64_t blocks = ((int64_t)p.paged.max_pages * p.paged.page_size + 15) / 16;
-  const int64_t most = std::min<int64_t>(items <= 7 ? kClusterMost : 10, (blocks + kWarps - 1) / kWarps);
-  return (int)std::max<int64_t>(1, std::min<int64_t>(256 / items, most));
+// Clusters only where all of them are resident at once with a CTA per SM (of 16, 10, 8, 4, 2 CTAs 7, 11, 15, 33, 74 are), and, with more
+// than one sequence, only over short caches: it is not known here how long they are, and one long sequence would be left to its clusters.
+// us, caches new to L2, 32 / 8 heads of 128 (clusters | shares | ranges, 6 us of them the events'): 4 sequences of 2500 rows 20 | 24 | 33,
+// of 8000 35 | 39 | 48, 6 of 1000 to 8000 52 | 40 | 45, of 30000 163 | 132 | 140, 16 of 300 17 | 20 | 26, of 1000 to 8000 92 | 94 | 75.
+int cluster_size(const AttnParams& p) {  // 0: shares or ranges
+  const int64_t items = decode_items(p), blocks = ((int64_t)p.paged.max_pages * p.paged.page_size + 15) / 16;
+  int n = 0;
+  for (const auto& fit : {std::pair<int, int>{148, 1}, {74, 2}, {33, 4}, {15, 8}, {11, 10}, {7, 16}})
+    if (items <= fit.first) n = fit.second;
+  if (n == 0) return 0;
+  n = (int)std::min<int64_t>(n, (blocks + kWarps - 1) / kWarps);
+  return p.paged.batch == 1 || blocks <= 10 * kWarps * n ? n : 0;
 }
+bool shares(const AttnParams& p) { return decode_items(p) <= 74; }  // two CTAs an item
 
 }  // namespace
 
@@ -680,6 +816,7 @@ int paged_decode_rows(const AttnParams& p) { return 16 / paged_decode_heads(p); 
 size_t paged_decode_ws_bytes(const AttnParams& p, cascade_dtype_t dtype, int rows) {
   if (cluster_size(p) > 0) return 0;
   const int columns = rows * paged_decode_heads(p) <= 8 ? 8 : 16, n = ranges_cta(dtype, p.d);
+  if (shares(p)) return (size_t)n * (columns * (p.d + 2) * 4 + sizeof(int4));
   return (size_t)n * (2 * columns * (p.d + 2) * 4 + sizeof(RangeStart));
 }
 
@@ -704,7 +841,19 @@ cudaError_t launch_paged_decode(const AttnParams& p, cascade_dtype_t dtype, int 
       a.n_cta = cluster;
       return launch_dependent(kernel, dim3(cluster, a.items, p.paged.batch), kThreads, smem, cluster, true, stream, p, a);
     }
-    constexpr int kAhead = (sizeof(T) == 2) == (D == 128) ? 2 : 1;
+    if (shares(p)) {
+      constexpr int kAhead = sizeof(T) == 4 && D == 128 ? 1 : 2;
+      a.n_cta = 148;
+      a.joins = static_cast<int4*>(workspace);
+      a.partials = reinterpret_cast<float*>(a.joins + a.n_cta);
+      auto kernel = paged_decode_shares_kernel<T, D, NT, kAhead>;
+      cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
+      if (e != cudaSuccess) return e;
+      e = launch_dependent(kernel, dim3(a.n_cta), kThreads, smem, 1, true, stream, p, a);
+      if (e != cudaSuccess) return e;
+      return launch_dependent(paged_decode_join_shares_kernel<T, D, NT>, dim3(a.n_cta, (rows * a.Gi * D + kJoinThreads - 1) / kJoinThreads), kJoinThreads, 0, 1, true, stream, p, a);
+    }
+    constexpr int kAhead = sizeof(T) == 2 ? (D == 128 && NT == 1 ? 2 : 1) : (D == 64 && NT == 1 ? 2 : 1);
     a.n_cta = ranges_cta(dtype, p.d);
     a.starts = static_cast<RangeStart*>(workspace);
     a.partials = reinterpret_cast<float*>(a.starts + a.n_cta);

@@ -16,7 +16,7 @@ class Batch:
     NaN, and the table's unused entries and the padded rows are garbage."""
 
     def __init__(self, rows, lens, H, Hkv, d, page, dtype=torch.bfloat16, seed=0, pad=3, head_major=False, lead=0, spare=3, scale_k=1.0,
-                 strided=False):
+                 strided=False, width=None):
         g = torch.Generator().manual_seed(seed)
         rng = np.random.default_rng(seed)
         self.rows, self.lens, self.H, self.Hkv, self.d, self.page, self.dtype = list(rows), list(lens), H, Hkv, d, page, dtype
@@ -24,7 +24,7 @@ class Batch:
         self.n = n
         self.starts = np.concatenate([[0], np.cumsum(rows)]) + lead
         counts = [-(-x // page) for x in lens]
-        self.n_pages, width = sum(counts) + spare, max(counts + [1]) + 1
+        self.n_pages, width = sum(counts) + spare, width or max(counts + [1]) + 1
         table = rng.choice([-7, 2 ** 30, 10 ** 6], (len(rows), width)).astype(np.int32)
         ids = rng.permutation(self.n_pages)
         at = 0

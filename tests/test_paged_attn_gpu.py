@@ -36,6 +36,23 @@ def test_single_tokens(dtype, d, H, Hkv, page):
 
 @pytest.mark.parametrize("dtype,d", TYPES)
 @pytest.mark.parametrize("H,Hkv", HEADS)
+@pytest.mark.parametrize("n", [2, 7, 37, 100])
+def test_tokens_and_drafts_behind_wide_tables(dtype, d, H, Hkv, n):
+    """Tables with room for 64000 rows, which nobody has: how the keys are shared out goes by the lengths on the device.  One sequence
+    is far longer than the others, some are empty, some have no new row, and the rows of the others are one to four."""
+    rng = np.random.default_rng(n + H)
+    lens = [int(x) for x in rng.integers(0, 90, n)]
+    lens[n // 2], lens[-1] = 1500 if H < 32 else 700, 0
+    news = [int(x) for x in rng.integers(1, 1 + max(1, min(4, 16 * Hkv // H)), n)]
+    if n > 3:
+        news[1] = 0
+    b = pu.Batch(news, lens, H, Hkv, d, 32, dtype, seed=n, width=2000)
+    attend(b, max_rows=4)
+    attend(b, causal=False, max_rows=4)
+
+
+@pytest.mark.parametrize("dtype,d", TYPES)
+@pytest.mark.parametrize("H,Hkv", HEADS)
 @pytest.mark.parametrize("causal", [True, False])
 def test_chunks_of_any_size(dtype, d, H, Hkv, causal):
     """Tokens, drafts, chunks and whole prompts side by side; sequences without new rows, without a cache, and with more new rows than
