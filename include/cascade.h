@@ -469,7 +469,9 @@ cascade_status_t cascade_decode_step_rope(cascade_plan_t* plan, int32_t batch, i
  * checked there before it forms an address.  A bad row_start counts as no rows, a bad length as the nearest good one, a bad page
  * id as page 0 (nothing is written to it); the first is kept for cascade_paged_status, and the outputs of its sequence are then
  * not to be used.
- * Two calls that write the same pages, or pages that the other reads, have to be ordered by the caller.
+ * New rows may only go to pages that one sequence holds (cascade_pages_fork sees to that).  Two calls that write the same pages, or
+ * pages that the other reads, have to be ordered by the caller.  Make a first paged call on each device before one is captured (it
+ * loads the kernels).  No sequence may have room for more than 2^30 rows.
  */
 
 /* Reads and clears what the paged calls on the current device have reported (SYNCHRONISES the device).  *out_code: 0, a code of

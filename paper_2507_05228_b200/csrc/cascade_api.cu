@@ -172,7 +172,7 @@ using namespace cascade;
 
 extern "C" {
 
-int32_t cascade_version(void) { return 101; }
+int32_t cascade_version(void) { return 102; }
 const char* cascade_last_error(void) { return g_err; }
 int64_t cascade_launch_count(void) { return g_launches.load(std::memory_order_relaxed); }
 

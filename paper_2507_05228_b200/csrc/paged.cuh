@@ -8,6 +8,13 @@
 
 namespace cascade {
 
+// A load of what the kernel in front may have written: an ordinary one.  These kernels start as programmatic dependents, before that one
+// is done, so what they read is not constant for as long as they run, which a load through the read-only path (__ldg) asks for.
+template <typename T>
+__device__ __forceinline__ T fresh(const T* p) {
+  return *p;
+}
+
 // Words 0 .. kStatusWords - 1: a bounded wait that gave up, as in a plan (WaitCtx).  Then a bad index: its code, the sequence (or
 // pair) and the value.
 enum PagedStatus { kBadIndexWord = 32, kPagedStatusWords = 36 };
@@ -29,7 +36,7 @@ __device__ __forceinline__ void paged_report(int32_t* status, int code, int wher
 
 // First row and number of rows of sequence b; none where row_start makes no sense.
 __device__ __forceinline__ int2 paged_rows(const PagedDev& g, int b) {
-  const int first = __ldg(g.row_start + b), end = __ldg(g.row_start + b + 1);
+  const int first = fresh(g.row_start + b), end = fresh(g.row_start + b + 1);
   if (first < 0 || end < first || end > g.n_rows) {
     paged_report(g.status, kBadRowStart, b, first);
     return make_int2(0, 0);
@@ -38,7 +45,7 @@ __device__ __forceinline__ int2 paged_rows(const PagedDev& g, int b) {
 }
 // Cache rows of sequence b, as many as its row of the table can hold.
 __device__ __forceinline__ int paged_len(const PagedDev& g, int b) {
-  const int len = __ldg(g.kv_len + b);
+  const int len = fresh(g.kv_len + b);
   const int64_t most = (int64_t)g.max_pages * g.page_size;
   if (len >= 0 && len <= most) return len;
   paged_report(g.status, kBadLength, b, len);
@@ -46,14 +53,14 @@ __device__ __forceinline__ int paged_len(const PagedDev& g, int b) {
 }
 // Id of page i of sequence b (i below max_pages); page 0 in the place of a bad one, which is reported.
 __device__ __forceinline__ int paged_page(const PagedDev& g, int b, int i) {
-  const int id = __ldg(g.table + (int64_t)b * g.table_stride + i);
+  const int id = fresh(g.table + (int64_t)b * g.table_stride + i);
   if ((unsigned)id < (unsigned)g.n_pages) return id;
   paged_report(g.status, kBadPage, b, id);
   return 0;
 }
 // Cache rows that row i of the n of a sequence sees; `row` is its place among all rows.
 __device__ __forceinline__ int paged_seen(const PagedDev& g, bool causal, int n, int len, int i, int row) {
-  if (g.visible) return max(0, min(len, __ldg(g.visible + row)));
+  if (g.visible) return max(0, min(len, fresh(g.visible + row)));
   return causal ? max(0, len - n + i + 1) : len;
 }
 
@@ -68,7 +75,7 @@ __device__ __forceinline__ int2 paged_tile(const PagedDev& g, int t, int per_til
     const int tiles = n >= g.least && n <= g.most ? (n + per_tile - 1) / per_tile : 0;
     const int total = __reduce_add_sync(0xffffffffu, tiles);
     if (t < before + total) {
-      const int len = tiles > 0 ? __ldg(g.kv_len + b) : INT_MIN;
+      const int len = tiles > 0 ? fresh(g.kv_len + b) : INT_MIN;
       int first = before;  // tiles of the sequences that come before this lane's
       for (int j = 0; j < min(32, g.batch - b0); ++j) {
         const int other = __shfl_sync(0xffffffffu, len, j), n_other = __shfl_sync(0xffffffffu, tiles, j);

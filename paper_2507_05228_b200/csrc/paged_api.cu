@@ -53,7 +53,7 @@ cascade_status_t check_sizes(const char* fn, int32_t H, int32_t Hkv, int32_t pag
     set_error("%s: page_size %d unsupported (a multiple of 16)", fn, page_size);
     return CASCADE_ERR_UNSUPPORTED;
   }
-  if ((int64_t)max_pages * page_size > INT32_MAX - 512) return fail(CASCADE_ERR_UNSUPPORTED, fn, "a sequence of more than 2^31 - 513 rows");
+  if ((int64_t)max_pages * page_size > 1 << 30) return fail(CASCADE_ERR_UNSUPPORTED, fn, "a sequence of more than 2^30 rows");
   return CASCADE_OK;
 }
 cascade_status_t check_pages(const char* fn, int32_t batch, int32_t n_rows, int32_t H, int32_t Hkv, int32_t n_pages, int32_t page_size,
@@ -378,7 +378,7 @@ static cascade_status_t check_tables(const char* fn, int32_t n_seqs, int32_t wid
                                      const void* b, const void* c, const void* d, const void* e, const void* f) {
   if (!a || !b || !c || !d || !e || !f) return fail(CASCADE_ERR_INVALID_ARG, fn, "null pointer");
   if (n_seqs < 1 || width < 1 || n_pages < 1 || page_size < 1) return fail(CASCADE_ERR_INVALID_ARG, fn, "sizes must be positive");
-  if ((int64_t)width * page_size > INT32_MAX - 512) return fail(CASCADE_ERR_UNSUPPORTED, fn, "a sequence of more than 2^31 - 513 rows");
+  if ((int64_t)width * page_size > 1 << 30) return fail(CASCADE_ERR_UNSUPPORTED, fn, "a sequence of more than 2^30 rows");
   if (a == b) return fail(CASCADE_ERR_INVALID_ARG, fn, "the new table may not be the old one");
   return CASCADE_OK;
 }

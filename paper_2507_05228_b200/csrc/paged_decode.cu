@@ -368,14 +368,14 @@ __device__ __forceinline__ void load_queries(Shared<T, D, NT>& sh, const AttnPar
   if constexpr (sizeof(T) == 2) {
 #pragma unroll
     for (int c = 0; c < D / 32; ++c) {
-      const uint4 t = q ? __ldg(reinterpret_cast<const uint4*>(q + 64 * (c >> 1) + 16 * j + 8 * (c & 1))) : make_uint4(0u, 0u, 0u, 0u);
+      const uint4 t = q ? fresh(reinterpret_cast<const uint4*>(q + 64 * (c >> 1) + 16 * j + 8 * (c & 1))) : make_uint4(0u, 0u, 0u, 0u);
       sh.q[warp].step[2 * c][lane] = make_uint2(t.x, t.y);
       sh.q[warp].step[2 * c + 1][lane] = make_uint2(t.z, t.w);
     }
   } else {
 #pragma unroll
     for (int c = 0; c < D / 16; ++c) {  // columns 32 (c / 2) + 8 j + 4 (c % 2) ..: two steps
-      const float4 t = q ? __ldg(reinterpret_cast<const float4*>(q + 32 * (c >> 1) + 8 * j + 4 * (c & 1))) : make_float4(0.f, 0.f, 0.f, 0.f);
+      const float4 t = q ? fresh(reinterpret_cast<const float4*>(q + 32 * (c >> 1) + 8 * j + 4 * (c & 1))) : make_float4(0.f, 0.f, 0.f, 0.f);
       uint4 f0, f1;
       cut_rounded(t.x, f0.x, f0.z);
       cut_rounded(t.y, f0.y, f0.w);

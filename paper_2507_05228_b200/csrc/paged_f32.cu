@@ -51,16 +51,17 @@ struct F32Cfg {
 
 template <int D, int MT, int RW, int KW>
 __global__ void __launch_bounds__(32 * RW * KW)
-paged_f32_kernel(const __grid_constant__ AttnParams p, int lg) {
+paged_f32_kernel(const __grid_constant__ AttnParams p, int lg, int tile_major) {
   using C = F32Cfg<D, MT, RW, KW>;
   extern __shared__ __align__(16) float smem[];
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, group = warp / RW, gtid = tid % (RW * 32);
   const int wrow = warp % RW * 16 * MT, g = lane >> 2, t = lane & 3;
   grid_go();
   grid_wait();
-  const int2 tile = paged_tile(p.paged, blockIdx.z, C::kRows >> lg, lane);
+  // tiles on the slowest axis, the longest first, unless there are too many for it
+  const int2 tile = paged_tile(p.paged, tile_major ? blockIdx.z : blockIdx.x, C::kRows >> lg, lane);
   if (tile.x < 0) return;
-  const int b = tile.x, key_part = blockIdx.y, h0 = blockIdx.x << lg, kv_head = h0 / p.G;
+  const int b = tile.x, key_part = tile_major ? blockIdx.y : blockIdx.z, h0 = (tile_major ? blockIdx.x : blockIdx.y) << lg, kv_head = h0 / p.G;
   const int2 rows = paged_rows(p.paged, b);
   const int len = paged_len(p.paged, b), tok0 = tile.y * (C::kRows >> lg), n_rows = min(C::kRows >> lg, rows.y - tok0) << lg;
   auto token_of = [&](int r) { return tok0 + (r >> lg); };
@@ -363,14 +364,14 @@ __global__ void __launch_bounds__(256) paged_combine_kernel(const __grid_constan
   const int64_t item = (int64_t)blockIdx.x * (256 / (D / 4)) + threadIdx.x / (D / 4);
   const int col = threadIdx.x % (D / 4) * 4;
   const int64_t all = (int64_t)p.paged.n_rows * p.H, row = item / p.H;
-  if (item >= all || row < __ldg(p.paged.row_start) || row >= __ldg(p.paged.row_start + p.paged.batch)) return;
+  if (item >= all || row < fresh(p.paged.row_start) || row >= fresh(p.paged.row_start + p.paged.batch)) return;
   float n = -INFINITY, w = 0.f;
   float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
-  for (int k = 0; k < p.key_parts; ++k) n = fmaxf(n, __ldg(p.m_part + k * all + item));
+  for (int k = 0; k < p.key_parts; ++k) n = fmaxf(n, fresh(p.m_part + k * all + item));
   for (int k = 0; k < p.key_parts; ++k) {
-    const float l = __ldg(p.l_part + k * all + item);
-    const float f = l > 0.f ? l * expf(__ldg(p.m_part + k * all + item) - n) : 0.f;
-    const float4 u = __ldg(reinterpret_cast<const float4*>(static_cast<const float*>(p.o_part) + (k * all + item) * D + col));
+    const float l = fresh(p.l_part + k * all + item);
+    const float f = l > 0.f ? l * expf(fresh(p.m_part + k * all + item) - n) : 0.f;
+    const float4 u = fresh(reinterpret_cast<const float4*>(static_cast<const float*>(p.o_part) + (k * all + item) * D + col));
     w += f;
     o.x = fmaf(f, u.x, o.x);
     o.y = fmaf(f, u.y, o.y);
@@ -408,7 +409,10 @@ cudaError_t launch_one(const AttnParams& p, cudaStream_t stream) {
   cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)C::kBytes);
   if (e != cudaSuccess) return e;
   const int lg = heads_log2(p.G);
-  return launch_dependent(kernel, dim3(p.H >> lg, p.key_parts, (unsigned)tiles_bound(p, C::kRows)), 32 * C::kWarps, C::kBytes, 1, true, stream, p, lg);
+  const unsigned heads = (unsigned)(p.H >> lg), parts = (unsigned)p.key_parts, tiles = (unsigned)tiles_bound(p, C::kRows);
+  const int tile_major = tiles <= 65535;
+  return launch_dependent(kernel, tile_major ? dim3(heads, parts, tiles) : dim3(tiles, heads, parts), 32 * C::kWarps, C::kBytes, 1, true, stream, p, lg,
+                          tile_major);
 }
 template <int D>
 cudaError_t launch_d(const AttnParams& p, cudaStream_t stream) {

@@ -122,17 +122,17 @@ __global__ void __launch_bounds__(kPagesThreads) pages_fork_kernel(const __grid_
   for (int i = gt; i < p.n_pages; i += all) holders.refs[i] = 0;
   if (gt < 4) p.report[gt] = 0;
   for (int i = tid; i < n; i += kPagesThreads) {
-    const int src = __ldg(p.source + i), add = __ldg(p.add + i);
+    const int src = fresh(p.source + i), add = fresh(p.add + i);
     int had = 0, last = -1;
     if (src < -1 || src >= n || add < 0) {
       atomicAdd(&s_bad, 1);
     } else if (src >= 0) {
-      had = __ldg(p.kv_in + src);
+      had = fresh(p.kv_in + src);
       if (pages_of(had, p) < 0) {
         had = 0;
         atomicAdd(&s_bad, 1);
       } else if (add > 0 && had % P > 0) {
-        last = __ldg(p.table_in + (int64_t)src * p.width + had / P);
+        last = fresh(p.table_in + (int64_t)src * p.width + had / P);
       }
     }
     if ((int64_t)had + max(add, 0) > (int64_t)p.width * P) atomicAdd(&s_long, 1);
@@ -145,7 +145,7 @@ __global__ void __launch_bounds__(kPagesThreads) pages_fork_kernel(const __grid_
   // holders of every page
   for_entries(n, p.width, gt, all, [&](int i, int c, int64_t) {
     if ((int64_t)c * P < s_had[i]) {
-      const int page = __ldg(p.table_in + (int64_t)s_src[i] * p.width + c);
+      const int page = fresh(p.table_in + (int64_t)s_src[i] * p.width + c);
       if ((unsigned)page < (unsigned)p.n_pages) atomicAdd(holders.refs + page, 1);
       else atomicAdd(kOne ? &s_ids : p.report + 2, 1);
     }
@@ -210,13 +210,13 @@ __global__ void __launch_bounds__(kPagesThreads) pages_fork_kernel(const __grid_
     for (int i = gt; i < p.n_pages; i += all) holders.refs[i] = 0;
     for (int i = gt; i < n; i += all) {
       *reinterpret_cast<int2*>(p.pairs + 2 * i) = make_int2(-1, -1);
-      p.kv_out[i] = __ldg(p.kv_in + i);
+      p.kv_out[i] = fresh(p.kv_in + i);
     }
     sync_all<kOne>();
     for_entries(n, p.width, gt, all, [&](int i, int c, int64_t e) {
-      const int page = __ldg(p.table_in + e);
+      const int page = fresh(p.table_in + e);
       p.table_out[e] = page;
-      if (c < pages_of(__ldg(p.kv_in + i), p) && (unsigned)page < (unsigned)p.n_pages) atomicAdd(holders.refs + page, 1);
+      if (c < pages_of(fresh(p.kv_in + i), p) && (unsigned)page < (unsigned)p.n_pages) atomicAdd(holders.refs + page, 1);
     });
     sync_all<kOne>();
     const int left = count_pages(first, end, s_warp, is_free);
@@ -249,7 +249,7 @@ __global__ void __launch_bounds__(kPagesThreads) pages_fork_kernel(const __grid_
     const int had = s_had[i];
     if ((int64_t)c * P < had) {
       if (s_own[i] && c == had / P) atomicSub(holders.refs + s_last[i], 1);  // it has a copy now
-      else p.table_out[e] = __ldg(p.table_in + (int64_t)s_src[i] * p.width + c);
+      else p.table_out[e] = fresh(p.table_in + (int64_t)s_src[i] * p.width + c);
     } else if ((int64_t)c * P >= (int64_t)had + s_add[i]) {
       p.table_out[e] = -1;
     }
@@ -280,10 +280,10 @@ __global__ void __launch_bounds__(kPagesThreads) pages_compact_kernel(const __gr
   sync_all<kOne>();
   int* const bad = kOne ? &s_bad : p.report + 2;
   for (int i = gt; i < p.n_seqs; i += all)
-    if (pages_of(__ldg(p.kv_in + i), p) < 0) atomicAdd(bad, 1);
+    if (pages_of(fresh(p.kv_in + i), p) < 0) atomicAdd(bad, 1);
   for_entries(p.n_seqs, p.width, gt, all, [&](int i, int c, int64_t e) {
-    const int page = __ldg(p.table_in + e);  // (asked for before the length is known)
-    if (c >= pages_of(__ldg(p.kv_in + i), p)) return;
+    const int page = fresh(p.table_in + e);  // (asked for before the length is known)
+    if (c >= pages_of(fresh(p.kv_in + i), p)) return;
     if ((unsigned)page < (unsigned)p.n_pages) atomicAdd(holders.refs + page, 1);
     else atomicAdd(bad, 1);
   });
@@ -299,7 +299,7 @@ __global__ void __launch_bounds__(kPagesThreads) pages_compact_kernel(const __gr
     for (int r = 0; r < n_cta; ++r) n_live += s_live[r];
   }
   if ((kOne ? s_bad : __ldcg(p.report + 2)) > 0) {  // nothing is moved
-    for_entries(p.n_seqs, p.width, gt, all, [&](int, int, int64_t e) { p.table_out[e] = __ldg(p.table_in + e); });
+    for_entries(p.n_seqs, p.width, gt, all, [&](int, int, int64_t e) { p.table_out[e] = fresh(p.table_in + e); });
     for (int i = gt; i < p.max_pairs; i += all) *reinterpret_cast<int2*>(p.pairs + 2 * i) = make_int2(-1, -1);
     if (gt == 0) {
       p.report[0] = n_live;
@@ -343,8 +343,8 @@ __global__ void __launch_bounds__(kPagesThreads) pages_compact_kernel(const __gr
   }
   sync_all<kOne>();
   for_entries(p.n_seqs, p.width, gt, all, [&](int i, int c, int64_t e) {
-    int page = __ldg(p.table_in + e);
-    if (c >= pages_of(__ldg(p.kv_in + i), p)) page = -1;
+    int page = fresh(p.table_in + e);
+    if (c >= pages_of(fresh(p.kv_in + i), p)) page = -1;
     else if (page >= n_live) page = -holders.get(page) - 1;
     p.table_out[e] = page;
   });
@@ -378,7 +378,7 @@ __global__ void __launch_bounds__(kCopyThreads) pages_copy_kernel(const __grid_c
     for (int j0 = 0; j0 < n_w; j0 += kCopyThreads) {
       const int j = j0 + tid;
       int2 e = make_int2(-1, -1);
-      if (j < n_w) e = make_int2(__ldg(p.pairs + 2 * (int64_t)(w0 + j)), __ldg(p.pairs + 2 * (int64_t)(w0 + j) + 1));
+      if (j < n_w) e = make_int2(fresh(p.pairs + 2 * (int64_t)(w0 + j)), fresh(p.pairs + 2 * (int64_t)(w0 + j) + 1));
       const bool none = e.x == -1 || e.y == -1;
       const bool fine = (unsigned)e.x < (unsigned)p.n_pages && (unsigned)e.y < (unsigned)p.n_pages;
       if (!none && !fine && blockIdx.x == 0) paged_report(p.status, kBadPair, w0 + j, (unsigned)e.x < (unsigned)p.n_pages ? e.y : e.x);

@@ -56,7 +56,7 @@ __device__ __forceinline__ int sequence_of(const PagedDev& g, int r, int lane) {
   int lo = 0, n = g.batch;  // the answer is in [lo, lo + n)
   while (n > 1) {
     const int step = (n + 31) / 32, at = lo + lane * step;
-    const bool starts = lane * step < n && __ldg(g.row_start + at) <= r;
+    const bool starts = lane * step < n && fresh(g.row_start + at) <= r;
     const uint32_t m = __ballot_sync(0xffffffffu, starts);
     if (m == 0) return -1;
     const int last = 31 - __clz(m);
@@ -112,16 +112,16 @@ __global__ void __launch_bounds__(256) rope_rows_kernel(const __grid_constant__ 
       return;
     }
     const int index = y / p.paged.page_size, slot = y - index * p.paged.page_size;
-    const int id = __ldg(p.paged.table + (int64_t)s * p.paged.table_stride + index);
+    const int id = fresh(p.paged.table + (int64_t)s * p.paged.table_stride + index);
     if ((unsigned)id >= (unsigned)p.paged.n_pages) {  // nothing is written
       if (lane == 0) paged_report(p.paged.status, kBadPage, s, id);
       return;
     }
     k_to = id * p.kos.batch + slot * p.kos.token;
     v_to = id * p.vos.batch + slot * p.vos.token;
-    position = p.positions ? __ldg(p.positions + row) : y;
+    position = p.positions ? fresh(p.positions + row) : y;
   } else {
-    position = __ldg(p.positions + row);
+    position = fresh(p.positions + row);
     if (position < 0) return;  // a padded row stays as it is
   }
   if (p.rope && (unsigned)position >= (unsigned)p.n_positions) {
@@ -132,7 +132,7 @@ __global__ void __launch_bounds__(256) rope_rows_kernel(const __grid_constant__ 
   if (turned) {
     const float4* t = reinterpret_cast<const float4*>(p.rope + (int64_t)position * half + u * N);
 #pragma unroll
-    for (int e = 0; e < N / 2; ++e) cs[e] = __ldg(t + e);
+    for (int e = 0; e < N / 2; ++e) cs[e] = fresh(t + e);
   }
 #pragma unroll
   for (int i = 0; i < kHeads; ++i) {

@@ -211,6 +211,67 @@ def test_the_same_call_gives_the_same_bits():
             assert torch.equal(o[:sum(news)], o2[:sum(news)]) and torch.equal(lse[:sum(news)], lse2[:sum(news)])
 
 
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("news", [[1, 2, 1], [1, 90, 300]])
+def test_layers_of_one_pool_and_strided_outputs(dtype, news):
+    """Pages of K and V of several layers in one tensor, a table that is part of a wider one, outputs and queries inside wider rows."""
+    b = pu.Batch(news, [100, 200, 310], 8, 2, 128, 16, dtype, seed=9, strided=True)
+    pool = torch.full((b.n_pages, 3, 2, 16, 2, 128), math.nan, dtype=dtype, device="cuda")
+    pool[:, 1, 0], pool[:, 1, 1] = b.k_pages, b.v_pages
+    b.k_pages, b.v_pages = pool[:, 1, 0], pool[:, 1, 1]
+    table = torch.full((3, 100), -5, dtype=torch.int32, device="cuda")
+    table[:, 20:20 + b.table.shape[1]] = b.table
+    b.table = table[:, 20:20 + b.table.shape[1]]
+    wide = torch.full((b.n, 12, 160), 7.0, dtype=dtype, device="cuda")
+    out = wide[:, 2:10, 16:144]
+    o, lse = cb.cascade_attn_paged(b.q, b.k_pages, b.v_pages, b.table, b.row_start, b.kv_len, b.scale, out=out)
+    assert cb.cascade_paged_status() == 0
+    b.check(o, lse)
+    wide[:, 2:10, 16:144] = 7.0
+    assert (wide[:sum(news)] == 7).all()
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("H,Hkv", [(21, 3), (20, 1), (34, 2), (64, 1)])
+def test_odd_groups_of_heads(dtype, H, Hkv):
+    for news, lens in (([1, 1, 2], [70, 33, 129]), ([40, 1, 3], [140, 33, 129])):
+        attend(pu.Batch(news, lens, H, Hkv, 64, 16, dtype, seed=H))
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("n,width", [(3, None), (3, 2000), (200, 2000)])
+def test_more_rows_than_announced_are_reported_and_left(dtype, n, width):
+    news = [1] * n
+    news[1] = 3
+    b = pu.Batch(news, [50 + i % 7 for i in range(n)], 8, 2, 64, 16, dtype, seed=1, width=width)
+    out = torch.full((b.n, 8, 64), 5.0, dtype=dtype, device="cuda")
+    cb.cascade_attn_paged(b.q, b.k_pages, b.v_pages, b.table, b.row_start, b.kv_len, b.scale, max_rows=1, out=out)
+    with pytest.raises(cb.CascadeError, match="code 126.*sequence 1, value 3"):
+        cb.cascade_paged_status()
+    o_ref, _, off, _ = b.reference()
+    others = [r for r in range(sum(news)) if r not in (1, 2, 3)]
+    assert ((out.double().cpu() - o_ref).abs() <= off)[others].all() and (out[1:4] == 5).all()
+
+
+def test_calls_on_several_streams_at_once():
+    """Chunks, tokens and fp32 side by side, again and again, each with its own outputs and workspace."""
+    cases = [pu.Batch([1] * 5, [300, 20, 900, 64, 1], 8, 2, 128, 16, seed=1), pu.Batch([70, 1, 200], [300, 20, 900], 8, 2, 128, 16, seed=2),
+             pu.Batch([3, 60], [300, 200], 8, 2, 64, 16, torch.float32, seed=3), pu.Batch([1, 1], [3000, 2000], 8, 2, 64, 32, seed=4, width=2000)]
+    streams = [torch.cuda.Stream() for _ in cases]
+    torch.cuda.synchronize()
+    got = [[] for _ in cases]
+    for _ in range(10):
+        for b, s, g in zip(cases, streams, got):
+            with torch.cuda.stream(s):
+                g.append(cb.cascade_attn_paged(b.q, b.k_pages, b.v_pages, b.table, b.row_start, b.kv_len, b.scale))
+    torch.cuda.synchronize()
+    assert cb.cascade_paged_status() == 0
+    for b, g in zip(cases, got):
+        b.check(*g[0])
+        n = sum(b.rows)
+        assert all(torch.equal(o[:n], g[0][0][:n]) and torch.equal(lse[:n], g[0][1][:n]) for o, lse in g[1:])
+
+
 def test_no_rows():
     b = pu.Batch([2], [3], 4, 2, 64, 16)
     o, lse = cb.cascade_attn_paged(b.q[:0], b.k_pages, b.v_pages, b.table[:0], b.row_start[:1], b.kv_len[:0], b.scale)

@@ -74,7 +74,7 @@ def test_append(L):
     for place in (1, 2, 3, 4, 23, 27, 16):
         refuses(f, args, 1, **{f"_{place}": 0})
     refuses(f, args, 1, _26=4)  # rows of the table closer together than they are long
-    refuses(f, args, 3, b"2^31", _24=1 << 30)
+    refuses(f, args, 3, b"2^30", _24=1 << 28)
     refuses(f, args, 1, b"aligned", _20=cb.Strides(16 * 512 + 4, 512, 128))
     refuses(f, args, 1, b"aligned", _10=P + 2)
     refuses(f, args, 1, _28=P + 2)
