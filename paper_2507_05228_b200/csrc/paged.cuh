@@ -52,11 +52,13 @@ __device__ __forceinline__ int paged_len(const PagedDev& g, int b) {
   return len < 0 ? 0 : (int)most;
 }
 // Id of page i of sequence b (i below max_pages); page 0 in the place of a bad one, which is reported.
-__device__ __forceinline__ int paged_page(const PagedDev& g, int b, int i) {
-  const int id = fresh(g.table + (int64_t)b * g.table_stride + i);
+__device__ __forceinline__ int paged_checked(const PagedDev& g, int b, int id) {
   if ((unsigned)id < (unsigned)g.n_pages) return id;
   paged_report(g.status, kBadPage, b, id);
   return 0;
+}
+__device__ __forceinline__ int paged_page(const PagedDev& g, int b, int i) {
+  return paged_checked(g, b, fresh(g.table + (int64_t)b * g.table_stride + i));
 }
 // Cache rows that row i of the n of a sequence sees; `row` is its place among all rows.
 __device__ __forceinline__ int paged_seen(const PagedDev& g, bool causal, int n, int len, int i, int row) {
