@@ -14,10 +14,10 @@
 // The pitches (D + 16 for keys, D + 4 for values) make all of these loads free of bank conflicts.
 //
 // RW warps share a tile of 32 keys, KW groups of them take the tiles in turn and add up in shared memory at the end: 64 rows a CTA
-// where that fills half the chip, 16 otherwise (16 rows a CTA in the example above: 40 us; 64 rows and two CTAs for the keys of each: 36).
+// where sequences have them, 16 otherwise (16 in the example above: 40 us).  Where CTAs are few, key_parts of them share the keys and
+// leave partials, which paged_combine_kernel adds up.
 // What bounds it: half the time of the CTA with the longest keys is its products (12288 of 8 cycles, four at a time), a fifth the
-// chain of look-ups and first loads.  Where rows are few, key_parts CTAs share the keys and leave partials, which
-// paged_combine_kernel adds up.
+// chain of look-ups and first loads.
 #include <algorithm>
 
 #include "paged.cuh"
@@ -397,10 +397,8 @@ int64_t tiles_bound(const AttnParams& p, int height) {
   const int per = height >> heads_log2(p.G);
   return p.paged.batch == 1 ? (p.paged.n_rows + per - 1) / per : p.paged.n_rows / per + p.paged.batch;
 }
-bool wide(const AttnParams& p) {
-  const int lg = heads_log2(p.G);
-  return (p.paged.n_rows / (64 >> lg)) * (int64_t)(p.H >> lg) >= kSms / 2;
-}
+// Sixty-four rows a CTA where a sequence has half of them on average
+bool wide(const AttnParams& p) { return (p.paged.n_rows / p.paged.batch) << heads_log2(p.G) >= 32; }
 
 template <int D, int MT, int RW, int KW>
 cudaError_t launch_one(const AttnParams& p, cudaStream_t stream) {
@@ -425,11 +423,11 @@ cudaError_t launch_d(const AttnParams& p, cudaStream_t stream) {
 
 }  // namespace
 
-// CTAs that fill the chip, each with at least 512 keys of what the table can hold.
+// A CTA per SM, each with at least 256 keys of what the table can hold (us, two CTAs per SM and 512 keys | now: 3 drafts of 2 to 6 rows over
+// 646 to 672, 32 / 8 heads of 128, 37 | 25; 100 rows over 2000, 16 / 8 heads of 64, 47 | 32; 28 over 4000, 12 heads of 128, 64 | 44).
 int paged_f32_parts(const AttnParams& p) {
-  if (wide(p)) return 1;
-  const int64_t ctas = tiles_bound(p, 16) * (p.H >> heads_log2(p.G)), keys = (int64_t)p.paged.max_pages * p.paged.page_size;
-  return (int)std::max<int64_t>(1, std::min<int64_t>({2 * kSms / std::max<int64_t>(1, ctas), keys / 512, 64}));
+  const int64_t ctas = tiles_bound(p, wide(p) ? 64 : 16) * (p.H >> heads_log2(p.G)), keys = (int64_t)p.paged.max_pages * p.paged.page_size;
+  return (int)std::max<int64_t>(1, std::min<int64_t>({kSms / std::max<int64_t>(1, ctas), keys / 256, 64}));
 }
 size_t paged_f32_ws_bytes(const AttnParams& p) {
   const int64_t parts = paged_f32_parts(p);
