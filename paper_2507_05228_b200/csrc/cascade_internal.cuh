@@ -305,7 +305,7 @@ int paged_decode_heads(const AttnParams& p);
 int paged_decode_rows(const AttnParams& p);
 size_t paged_decode_ws_bytes(const AttnParams& p, cascade_dtype_t dtype, int rows);
 cudaError_t launch_paged_decode(const AttnParams& p, cascade_dtype_t dtype, int rows, void* workspace, cudaStream_t stream);
-cudaError_t launch_paged_tc(const AttnParams& p, cudaStream_t stream);
+cudaError_t launch_paged_tc(const AttnParams& p, int max_rows, cudaStream_t stream);
 
 // Rows turned by their positions and, with pages, appended (cascade_rope_rows, cascade_paged_append)
 struct RopeRowsParams {

@@ -364,7 +364,7 @@ cascade_status_t cascade_attn_paged(cascade_dtype_t dtype, int32_t batch, int32_
   if (r.tiles) {
     AttnParams many = p;
     many.paged.least = r.rows + 1;
-    e = dtype == CASCADE_BF16 ? launch_paged_tc(many, st) : launch_paged_f32(many, workspace, st);
+    e = dtype == CASCADE_BF16 ? launch_paged_tc(many, max_rows, st) : launch_paged_f32(many, workspace, st);
   }
   if (e == cudaSuccess && r.rows > 0) {
     p.paged.most = r.rows;
