@@ -1629,11 +1629,12 @@ cudaError_t launch_paged_tc(const AttnParams& p, int max_rows, cudaStream_t stre
   rows.plan.n_q = g.n_rows;
   tma.q_valid = encode_queries(&tma.q, rows, lg);
   // Every sequence can end in a tile that is not full.  The rules below go by the fewest tiles there can be: those of the rows, and one of
-  // every sequence that has more rows than the decode kernel takes (16 sequences of 6 rows over 3000 to 9000, 32 / 8 heads: in clusters
-  // of four by the rows alone 134 us, so 99).
+  // every sequence that has more rows than the decode kernel takes (4 sequences of 6 rows over 3000 to 9000, 32 / 8 heads: in clusters
+  // of eight by the rows alone 85 us, so 51).
   const int64_t per = 256 >> lg, few = p.paged.least - 1, over = std::max<int64_t>(0, g.n_rows - g.batch * few);
   const int64_t seqs = (over + std::max<int64_t>(1, max_rows - few) - 1) / std::max<int64_t>(1, max_rows - few);
-  const int64_t least = std::max((g.n_rows + per - 1) / per, std::min<int64_t>(g.batch, seqs)), bound = g.batch == 1 ? (g.n_rows + per - 1) / per : std::min<int64_t>(g.n_rows, g.n_rows / per + g.batch);
+  const int64_t least = std::max((g.n_rows + per - 1) / per, std::min<int64_t>(g.batch, seqs));
+  const int64_t bound = g.batch == 1 ? (g.n_rows + per - 1) / per : std::min<int64_t>(g.n_rows, g.n_rows / per + g.batch);
   const int64_t heads = p.H >> lg, key_tiles = ((int64_t)g.max_pages * g.page_size + 127) / 128;
   int lg_split = 0;  // as launch_attn_tc, by the keys that the table can hold
   const int64_t fit[4] = {148, 148, 132, 120};

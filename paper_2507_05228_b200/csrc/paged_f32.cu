@@ -6,8 +6,9 @@
 // products by themselves; what is carried from tile to tile is added in fp32.  (With the small products in the same sums the error of
 // the output was 7.8e-7, so it is 3.1e-7; the same in fp32 on the ALUs 4.1e-7.)
 //
-// A warp owns 16 rows (or 32, MT = 2: one cut of a key or value for two products each), (token, head) pairs with the heads of a KV head side by side.  The contraction index of a product may be any
-// permutation as long as both operands use the same one, and so may the output columns; with (g, t) = (lane / 4, lane % 4):
+// A warp owns 16 rows (or 32, MT = 2: one cut of a key or value for two products each), (token, head) pairs with the heads of a KV
+// head side by side.  The contraction index of a product may be any permutation as long as both operands use the same one, and so
+// may the output columns; with (g, t) = (lane / 4, lane % 4):
 //   q k^T  a lane's four columns 16 c + 4 t .. + 3 of a row are the indices t and t + 4 of two products: one 16-byte load
 //   p v    the logits of keys 2 t and 2 t + 1, which a lane holds, are the indices t and t + 4 of the weights, so nothing is moved;
 //          values are columns 4 g + 32 j .. + 3 of rows 2 t and 2 t + 1: one 16-byte load for four products

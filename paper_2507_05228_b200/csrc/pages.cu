@@ -7,7 +7,7 @@
 // shared memory.  A page is free when no sequence holds it, so the holders are counted anew every time and no list of free pages
 // has to be kept.  No list is written either: whoever ranks a free page looks up who takes the page of that rank.  Where the holders
 // fit in the shared memory of one CTA (kOne), that CTA does it alone, without a barrier or a trip to L2 between the steps (64
-// sequences, 1800 pages: fork 10 -> us, compaction -> ).
+// sequences, 1800 pages: a fork with its copies 17.2 us by a cluster, so 14.5).
 // Copying is bound by HBM: twice the bytes of the pages.
 #include <limits.h>
 

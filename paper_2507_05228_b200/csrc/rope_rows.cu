@@ -84,7 +84,7 @@ __global__ void __launch_bounds__(256) rope_rows_kernel(const __grid_constant__ 
   const bool turned = p.rope && u * 2 * N < p.rot;
   const int c0 = turned && !p.interleaved ? u * N : u * 2 * N, c1 = turned && !p.interleaved ? half + u * N : c0 + N;
   // The rows are asked for before it is known where they go: what has to be looked up for that (sequence, length, page, position) is
-  // a chain of loads as long as their own (3153 rows of 48 heads 16.9 us behind it, so 14.5).
+  // a chain of loads as long as their own (3153 rows of 48 heads 15.6 us behind it, so 13.9).
   const T* src[kHeads];
   uint4 a[kHeads], b[kHeads];
   const int heads = p.H + (kAppend ? 2 * p.Hkv : 0);
@@ -200,7 +200,7 @@ namespace {
 // cos and sin are multiplied by `attention`.
 // The angles of one position come with the launch (their powers were a third of the time on the device).  A thread has one dimension
 // and kRun positions: the first and the step go through sincos, the others are products, (cos, sin)(t + 1) = (cos, sin)(t) (cos,
-// sin)(1) as complex numbers, off by a few 2^-53 each.  (32768 positions of 64 pairs: 61 us with a power and a sincos for each, now 7.)
+// sin)(1) as complex numbers, off by a few 2^-53 each.  (32768 positions of 64 pairs: 61 us with a power and a sincos for each, now 6.2.)
 constexpr int kRun = 16, kMaxPairs = 128;
 struct RopeAngles {
   double theta[kMaxPairs];
