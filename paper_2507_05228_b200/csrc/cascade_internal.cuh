@@ -299,10 +299,11 @@ size_t paged_f32_ws_bytes(const AttnParams& p);
 cudaError_t launch_paged_f32(AttnParams p, void* workspace, cudaStream_t stream);
 // bf16 on the tensor cores, where a tensor map holds the pages
 bool paged_tc_takes(const AttnParams& p);
-// sequences of at most paged_decode_rows() rows: heads of an item, scratch for sequences of at most `rows` rows, the launch
-// (p.alone: sequences of more rows than p.paged.most are nobody's, and reported)
-int paged_decode_heads(const AttnParams& p);
-int paged_decode_rows(const AttnParams& p);
+// sequences of at most `rows` rows: heads of an item, scratch, the launch (p.alone: sequences of more rows than p.paged.most are
+// nobody's, and reported); paged_decode_rows(): rows up to which the heads of an item are not split for their sake
+int paged_decode_heads(const AttnParams& p, cascade_dtype_t dtype, int rows);
+int paged_decode_rows(const AttnParams& p, cascade_dtype_t dtype);
+bool paged_decode_splits(const AttnParams& p, cascade_dtype_t dtype, int rows);
 size_t paged_decode_ws_bytes(const AttnParams& p, cascade_dtype_t dtype, int rows);
 cudaError_t launch_paged_decode(const AttnParams& p, cascade_dtype_t dtype, int rows, void* workspace, cudaStream_t stream);
 cudaError_t launch_paged_tc(const AttnParams& p, int max_rows, cudaStream_t stream);

@@ -2,17 +2,23 @@
 // the bound is HBM for large batches and latency for small ones.
 //
 // The columns of warp-level mma.m16n8k16 products are (row, head) pairs: the rows of a sequence times the heads of a KV head (as many
-// as divide its group, 16 at most), 8 or 16 of them.  A warp walks blocks of 16 keys, which lie in one page, with the fragments
-// straight from global memory, as decode.cu does and says why.  The weights go into the second product as two bf16 parts, the upper
-// 16 bits and the rest, so that they keep 16 bits of mantissa: the loads are the limit, and with one part the rounding of few rows
-// of weights was most of the error (2500 rows, 32 heads: 2.4e-3 of the output, 1.7e-3 with two, which is its own rounding).
+// as divide its group, 16 at most), 8 to 32 of them.  A warp walks blocks of 16 keys, which lie in one page.
+//   Up to 8 columns the fragments come straight from global memory, as in decode.cu, which says why.
+//   More leave no registers for rows on their way.  Every warp then has a ring of 24 KiB in shared memory, filled by TMA a block at a
+//   time (two requests of 16 rows each), and reads fragments by ldmatrix.  It waits for its own copies only; no warp waits for another.
+//   us, 32 / 8 heads of 128, 16 sequences over 3000 to 9000 rows (bytes: 61): 2 rows each 83, 4 89, 6 98, 8 119; before, from registers 83
+//   and 109, and from 5 rows on in tiles of 256 that are nearly empty 131.  Over 3000 to 9000, 4 sequences of 6 rows 52 -> 32.
+// The weights go into the second product as two bf16 parts, the upper 16 bits and the rest, so that they keep 16 bits of mantissa: the
+// loads are the limit, and with one part the rounding of few rows of weights was most of the error (2500 rows, 32 heads: 2.4e-3 of
+// the output, 1.7e-3 with two, which is its own rounding).  From 17 columns on the products are the limit: one part, rounded to nearest,
+// as in the tile kernel (16 sequences of 6 rows 108 -> 98 us, of 8 136 -> 119).
 //
 // fp32 the same way with m16n8k8 products of operands cut into two tf32 parts (tf32.cuh); weights go from the lanes of their keys to
 // those of their columns by shuffles, and every block's products with the values are summed by themselves and added in fp32.
 //
 // How the keys are shared out (rules and times at cluster_size).  Lengths differ between sequences, and only the device knows them.
 //   Few (sequence, KV head) items over short caches, or one sequence: a cluster of CTAs has one and adds up in distributed shared
-//   memory; one launch.
+//   memory; one launch.  So have many over caches that cannot be long, in clusters of one that come in turns.
 //   Few otherwise: every item gets a CTA, and the other CTAs of the chip go to the items by their length; what the CTAs of an item
 //   leave is added up by a second, small kernel.
 //   Many: the 16-key blocks of all items, one after another, are cut into as many equal ranges as CTAs are resident; an item that a
@@ -24,6 +30,7 @@
 
 #include "decode_common.cuh"
 #include "paged.cuh"
+#include "tcgen05.cuh"
 #include "tf32.cuh"
 
 namespace cascade {
@@ -33,6 +40,7 @@ namespace {
 constexpr int kWarps = 8, kThreads = kWarps * 32, kJoinThreads = 128;
 constexpr int kMaxGroups = 2048;  // groups of 32 sequences
 constexpr int kClusterMost = 16;
+constexpr int kMostInRegisters = 8, kMostColumns = 32;
 
 // Where a CTA's range starts: the item that holds its first block, and that block's place in the item.
 struct RangeStart {
@@ -69,16 +77,73 @@ template <int D>
 struct Fragments<float, D> {
   uint4 step[D / 8][32];
 };
-template <typename T, int D, int NT>
+
+// More than kMostInRegisters columns leave no registers for the rows of the cache: they come to shared memory by TMA then, every warp
+// a ring of its own blocks.
+template <typename T, int NT>
+constexpr bool kStaged = sizeof(T) == 2 && NT > kMostInRegisters / 8;
+template <int D>
+constexpr int kStages = 384 / D;  // blocks of a warp's ring, 24 KiB
+template <int D>
+constexpr int kPartBytes = 16 * D * 2;  // keys or values of a block: boxes of 16 rows and 64 columns, 128-byte swizzle
+
+template <typename T, int D, int NT, bool kStaged>
 struct Shared {
   float o[kWarps][8 * NT][D + 4];
   float m[kWarps][8 * NT], l[kWarps][8 * NT];
   Fragments<T, D> q[NT];
+  __device__ __forceinline__ float* out(int warp, int col) { return o[warp][col]; }
+  __device__ __forceinline__ const float* out(int warp, int col) const { return o[warp][col]; }
 };
+template <typename T, int D, int NT>
+struct Shared<T, D, NT, true> {
+  uint8_t ring[kWarps][kStages<D>][2][kPartBytes<D>];  // and a warp's outputs, once it has walked all its blocks
+  float m[kWarps][8 * NT], l[kWarps][8 * NT];
+  Fragments<T, D> q[NT];
+  uint64_t full[kWarps][kStages<D>];
+  int words[2 + kWarps];  // WaitCtx
+  static_assert(8 * NT * (D + 4) * 4 <= kStages<D> * 2 * kPartBytes<D>, "a warp's outputs lie in its ring");
+  __device__ __forceinline__ float* out(int warp, int col) { return reinterpret_cast<float*>(ring[warp][0][0]) + col * (D + 4); }
+  __device__ __forceinline__ const float* out(int warp, int col) const { return reinterpret_cast<const float*>(ring[warp][0][0]) + col * (D + 4); }
+};
+template <typename T, int D, int NT>
+using SharedOf = Shared<T, D, NT, kStaged<T, NT>>;
+template <typename T, int D, int NT>
+constexpr int kSmemBytes = (int)sizeof(SharedOf<T, D, NT>) + (kStaged<T, NT> ? 1024 : 0);  // the ring starts at a multiple of 1024
+
+struct alignas(64) PageMaps {
+  CUtensorMap k, v;  // [page][head][64-column half][row of the page][64 columns]
+};
+struct NoMaps {};
+template <typename T, int NT>
+using MapsOf = std::conditional_t<kStaged<T, NT>, PageMaps, NoMaps>;
+
+template <typename T, int D, int NT>
+__device__ __forceinline__ SharedOf<T, D, NT>& shared_of(uint8_t* smem) {
+  if constexpr (kStaged<T, NT>) smem += (0u - tc::smem_u32(smem)) & 1023u;
+  return *reinterpret_cast<SharedOf<T, D, NT>*>(smem);
+}
+// (every warp its own barriers; the words are there after the next __syncthreads)
+template <typename T, int D, int NT>
+__device__ __forceinline__ void set_up(SharedOf<T, D, NT>& sh, int warp, int lane) {
+  if constexpr (kStaged<T, NT>) {
+    if (warp == 0 && lane < 2 + kWarps) sh.words[lane] = 0;
+    if (lane == 0)
+      for (int i = 0; i < kStages<D>; ++i) tc::mbar_init(tc::smem_u32(&sh.full[warp][i]), 1);
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+  }
+}
+// A bounded wait has given up, here or in an earlier call: nothing is written.
+template <typename T, int NT>
+__device__ __forceinline__ bool gave_up(const AttnParams& p) {
+  if constexpr (kStaged<T, NT>) return *reinterpret_cast<volatile const int32_t*>(p.paged.status) != 0;
+  return false;
+}
 
 template <int D, int NT>
 struct State {
-  float o[NT][D / 16][4];      // o[t][e][2 r + h]: column 8 t + 2 j + h, output column x D / 8 + 2 e + r
+  // o[t][e][2 r + h]: column 8 t + 2 j + h, output column x D / 8 + 2 e + r (staged: 16 e + 8 r + x)
+  float o[NT][D / 16][4];
   float m[NT][2], l[NT][2];    // log2 units; l: this thread's share
 };
 
@@ -87,7 +152,7 @@ template <typename T, int D, int NT>
 struct Walk {
   const AttnParams& p;
   const T *kp, *vp;  // this lane's columns of the KV head
-  int b, len, lane;
+  int b, g, len, lane;  // g: KV head
   float cs;
   int lim[NT][2];  // keys that this lane's columns see
 
@@ -123,6 +188,32 @@ struct Walk {
     return rescale;
   }
 
+  // bf16 weights of keys x and x + 8, transposed: upper 16 bits and the rest; or, of one part, rounded
+  static constexpr int kParts = NT > 2 ? 1 : 2;
+  static __device__ __forceinline__ void weights(const float (&w)[NT][4], uint32_t (&pa)[NT][kParts], uint32_t (&pb)[NT][kParts]) {
+    auto rest = [](float y) { return y - __uint_as_float(__float_as_uint(y) & 0xffff0000u); };
+#pragma unroll
+    for (int nt = 0; nt < NT; ++nt) {
+      if constexpr (kParts == 1) {
+        pa[nt][0] = transpose8(pack2_bf16(w[nt][0], w[nt][1]));
+        pb[nt][0] = transpose8(pack2_bf16(w[nt][2], w[nt][3]));
+        continue;
+      }
+      pa[nt][0] = transpose8(__byte_perm(__float_as_uint(w[nt][0]), __float_as_uint(w[nt][1]), 0x7632));
+      pb[nt][0] = transpose8(__byte_perm(__float_as_uint(w[nt][2]), __float_as_uint(w[nt][3]), 0x7632));
+      pa[nt][kParts - 1] = transpose8(pack2_bf16(rest(w[nt][0]), rest(w[nt][1])));
+      pb[nt][kParts - 1] = transpose8(pack2_bf16(rest(w[nt][2]), rest(w[nt][3])));
+    }
+  }
+  static __device__ __forceinline__ void scale_all(State<D, NT>& st, const float (&alpha)[NT][2]) {
+#pragma unroll
+    for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+      for (int e = 0; e < D / 16; ++e)
+#pragma unroll
+        for (int c = 0; c < 4; ++c) st.o[nt][e][c] *= alpha[nt][c & 1];
+  }
+
   // bf16: registers of a block's rows, and what is done with them
   struct RowsBf16 {
     uint32_t ka[D / 8], kb[D / 8], v[4][D / 16];
@@ -148,31 +239,17 @@ struct Walk {
         }
     }
     __device__ __forceinline__ void add(State<D, NT>& st, const float (&w)[NT][4], const float (&alpha)[NT][2], bool rescale, int) const {
-      uint32_t pa[NT][2], pb[NT][2];  // weights of keys x and x + 8, transposed; upper 16 bits and the rest
-      auto rest = [](float y) { return y - __uint_as_float(__float_as_uint(y) & 0xffff0000u); };
-#pragma unroll
-      for (int nt = 0; nt < NT; ++nt) {
-        pa[nt][0] = transpose8(__byte_perm(__float_as_uint(w[nt][0]), __float_as_uint(w[nt][1]), 0x7632));
-        pb[nt][0] = transpose8(__byte_perm(__float_as_uint(w[nt][2]), __float_as_uint(w[nt][3]), 0x7632));
-        pa[nt][1] = transpose8(pack2_bf16(rest(w[nt][0]), rest(w[nt][1])));
-        pb[nt][1] = transpose8(pack2_bf16(rest(w[nt][2]), rest(w[nt][3])));
-      }
-      if (__any_sync(0xffffffffu, rescale)) {
-#pragma unroll
-        for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
-          for (int e = 0; e < D / 16; ++e)
-#pragma unroll
-            for (int c = 0; c < 4; ++c) st.o[nt][e][c] *= alpha[nt][c & 1];
-      }
+      uint32_t pa[NT][kParts], pb[NT][kParts];
+      weights(w, pa, pb);
+      if (__any_sync(0xffffffffu, rescale)) scale_all(st, alpha);
 #pragma unroll
       for (int e = 0; e < D / 16; ++e) {
         const uint32_t a0 = __byte_perm(v[0][e], v[1][e], 0x5410), a1 = __byte_perm(v[0][e], v[1][e], 0x7632);
         const uint32_t a2 = __byte_perm(v[2][e], v[3][e], 0x5410), a3 = __byte_perm(v[2][e], v[3][e], 0x7632);
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt) {
-          mma_16816(st.o[nt][e], a0, a1, a2, a3, pa[nt][0], pb[nt][0]);
-          mma_16816(st.o[nt][e], a0, a1, a2, a3, pa[nt][1], pb[nt][1]);
+#pragma unroll
+          for (int i = 0; i < kParts; ++i) mma_16816(st.o[nt][e], a0, a1, a2, a3, pa[nt][i], pb[nt][i]);
         }
       }
     }
@@ -259,9 +336,124 @@ struct Walk {
   };
   using Rows = std::conditional_t<sizeof(T) == 2, RowsBf16, RowsF32>;
 
+  // bf16 rows in shared memory, fragments by ldmatrix: key (or value row) and 16-byte chunk of lane l's address, and what of it is fixed
+  static __device__ __forceinline__ uint32_t k_at(int lane) {
+    const int key = (lane & 7) + ((lane >> 3) & 1) * 8;
+    return key * 128 + (((lane >> 4) ^ (key & 7)) << 4);
+  }
+  static __device__ __forceinline__ uint32_t v_at(int lane) {
+    const int key = (lane & 7) + (lane >> 4) * 8;
+    return key * 128 + ((((lane >> 3) & 1) ^ (key & 7)) << 4);
+  }
+  static __device__ __forceinline__ uint32_t chunk_at(uint32_t at, int step) {  // of 16 columns
+    return (at ^ ((step & 3) << 5)) + (step >> 2) * 2048;
+  }
+  // (given up: copies in flight still write to shared memory; about a second at most)
+  static __device__ __forceinline__ void landed(uint32_t bar, uint32_t parity) {
+    const uint64_t t0 = tc::global_timer_ns();
+    while (!tc::mbar_try_wait(bar, parity) && tc::global_timer_ns() - t0 < 1000000000ull) {
+    }
+  }
+  // The same walk over rows that TMA brings.  `used`: blocks that the warp's ring has had.
+  template <typename Shared, typename Ready>
+  __device__ __forceinline__ void run_staged(State<D, NT>& st, Shared& sh, const PageMaps& maps, uint32_t& used, int warp, int first, int stride,
+                                             int count, Ready ready, const int* early = nullptr) const {
+    constexpr int S = kStages<D>;
+    const tc::WaitCtx<false, kWarps> wc{tc::smem_u32(sh.words), p.paged.status};
+    int pages = lane >= count ? 0 : early ? paged_checked(p.paged, b, *early) : page_of(first + lane * stride), pages_next = 0;
+    auto page_at = [&](int t) {  // (asked in order)
+      if ((t & 31) == 0 && t > 0) pages = pages_next;
+      if ((t & 31) == 16) pages_next = (t & ~31) + 32 + lane < count ? page_of(first + ((t & ~31) + 32 + lane) * stride) : 0;
+      return __shfl_sync(0xffffffffu, pages, t & 31);
+    };
+    auto request = [&](int t, int page) {
+      if (lane != 0) return;
+      const uint32_t u = (used + t) % S, bar = tc::smem_u32(&sh.full[warp][u]), to = tc::smem_u32(sh.ring[warp][u][0]);
+      const int slot = (first + t * stride) * 16 % p.paged.page_size;
+      tc::mbar_expect_tx(bar, 2 * kPartBytes<D>);
+      auto load = [&](uint32_t dst, const CUtensorMap* map) {
+        asm volatile("cp.async.bulk.tensor.5d.shared::cta.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %2, %4, %5}], [%6];" ::"r"(dst),
+                     "l"(map), "r"(0), "r"(slot), "r"(g), "r"(page), "r"(bar)
+                     : "memory");
+      };
+      load(to, &maps.k);
+      load(to + kPartBytes<D>, &maps.v);
+    };
+    if (lane == 0) asm volatile("fence.proxy.async.shared::cta;" ::: "memory");  // behind what the ring was used for before
+#pragma unroll
+    for (int a = 0; a < S; ++a)
+      if (a < count) request(a, page_at(a));
+    ready();
+#pragma unroll 1
+    for (int t = 0; t < count; ++t) {
+      const uint32_t u = (used + t) % S;
+      if (!__all_sync(0xffffffffu, tc::wait_bar(wc, tc::smem_u32(&sh.full[warp][u]), ((used + t) / S) & 1, 13, t))) {
+        if (lane == 0)
+          for (int i = t; i < min(count, t + S); ++i) landed(tc::smem_u32(&sh.full[warp][(used + i) % S]), ((used + i) / S) & 1);
+        break;
+      }
+      const int k0 = (first + t * stride) * 16;
+      const uint32_t keys = tc::smem_u32(sh.ring[warp][u][0]), values = keys + kPartBytes<D>;
+      float sc[NT][4], alpha[NT][2];
+#pragma unroll
+      for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) sc[nt][i] = 0.f;
+#pragma unroll
+      for (int i = 0; i < D / 16; ++i) {
+        uint32_t f[4];
+        asm volatile("ldmatrix.sync.aligned.m8n8.x4.shared.b16 {%0, %1, %2, %3}, [%4];"
+                     : "=r"(f[0]), "=r"(f[1]), "=r"(f[2]), "=r"(f[3])
+                     : "r"(keys + chunk_at(k_at(lane), i))
+                     : "memory");
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt) {
+          const uint2 q = sh.q[nt].step[i][lane];
+          mma_16816(sc[nt], f[0], f[1], f[2], f[3], q.x, q.y);
+        }
+      }
+      if (k0 + 16 > len) {  // rows behind the last one may hold anything: their weights are 0, and 0 times them has to be
+        for (int i = lane; i < (16 - (len - k0)) * (D / 8); i += 32) {
+          const int row = len - k0 + i / (D / 8), c = i % (D / 8);
+          asm volatile("st.shared.v4.b32 [%0], {%1, %1, %1, %1};" ::"r"(values + (c >> 3) * 2048 + row * 128 + ((c & 7) << 4)), "r"(0) : "memory");
+        }
+        __syncwarp();
+      }
+      const bool rescale = weigh(st, sc, alpha, k0);
+      uint32_t pa[NT][kParts], pb[NT][kParts];
+      weights(sc, pa, pb);
+      if (__any_sync(0xffffffffu, rescale)) scale_all(st, alpha);
+#pragma unroll
+      for (int e = 0; e < D / 16; ++e) {
+        uint32_t f[4];
+        asm volatile("ldmatrix.sync.aligned.m8n8.x4.trans.shared.b16 {%0, %1, %2, %3}, [%4];"
+                     : "=r"(f[0]), "=r"(f[1]), "=r"(f[2]), "=r"(f[3])
+                     : "r"(values + chunk_at(v_at(lane), e))
+                     : "memory");
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt) {
+#pragma unroll
+          for (int i = 0; i < kParts; ++i) mma_16816(st.o[nt][e], f[0], f[1], f[2], f[3], pa[nt][i], pb[nt][i]);
+        }
+      }
+      const int page = t + S < count ? page_at(t + S) : 0;
+      __syncwarp();
+      if (t + S < count) request(t + S, page);
+    }
+    used += max(count, 0);
+    __syncwarp();  // the ring may be written
+  }
+
   // blocks first, first + stride, .. (count of them)
   template <int kAhead, typename Ready>
-  __device__ __forceinline__ void run(State<D, NT>& st, const Fragments<T, D> (&q)[NT], int first, int stride, int count, Ready ready, const int* early = nullptr) const {
+  __device__ __forceinline__ void run(State<D, NT>& st, SharedOf<T, D, NT>& sh, const MapsOf<T, NT>& maps, uint32_t& used, int warp, int first,
+                                      int stride, int count, Ready ready, const int* early = nullptr) const {
+    if constexpr (kStaged<T, NT>) run_staged(st, sh, maps, used, warp, first, stride, count, ready, early);
+    else run_registers<kAhead>(st, sh.q, first, stride, count, ready, early);
+  }
+  template <int kAhead, typename Ready>
+  __device__ __forceinline__ void run_registers(State<D, NT>& st, const Fragments<T, D> (&q)[NT], int first, int stride, int count, Ready ready,
+                                                const int* early = nullptr) const {
     if (count <= 0) {
       ready();
       return;
@@ -321,7 +513,7 @@ struct Walk {
 };
 
 template <typename T, int D, int NT>
-__device__ __forceinline__ void publish(Shared<T, D, NT>& sh, const State<D, NT>& st, int warp, int lane) {
+__device__ __forceinline__ void publish(SharedOf<T, D, NT>& sh, const State<D, NT>& st, int warp, int lane) {
   const int x = lane >> 2, j = lane & 3;
 #pragma unroll
   for (int nt = 0; nt < NT; ++nt)
@@ -336,13 +528,20 @@ __device__ __forceinline__ void publish(Shared<T, D, NT>& sh, const State<D, NT>
         sh.l[warp][col] = l;
       }
 #pragma unroll
-      for (int e = 0; e < D / 16; ++e)
-        *reinterpret_cast<float2*>(&sh.o[warp][col][x * (D / 8) + 2 * e]) = make_float2(st.o[nt][e][h], st.o[nt][e][2 + h]);
+      for (int e = 0; e < D / 16; ++e) {
+        float* o = sh.out(warp, col);
+        if constexpr (kStaged<T, NT>) {
+          o[16 * e + x] = st.o[nt][e][h];
+          o[16 * e + 8 + x] = st.o[nt][e][2 + h];
+        } else {
+          *reinterpret_cast<float2*>(o + x * (D / 8) + 2 * e) = make_float2(st.o[nt][e][h], st.o[nt][e][2 + h]);
+        }
+      }
     }
 }
 // Output column c of column `col`: maximum, sum of weights and weighted sum over the warps
 template <typename T, int D, int NT>
-__device__ __forceinline__ void combine_warps(const Shared<T, D, NT>& sh, int col, int c, float& n, float& w, float& acc) {
+__device__ __forceinline__ void combine_warps(const SharedOf<T, D, NT>& sh, int col, int c, float& n, float& w, float& acc) {
   n = -INFINITY;
 #pragma unroll
   for (int i = 0; i < kWarps; ++i) n = fmaxf(n, sh.m[i][col]);
@@ -352,7 +551,7 @@ __device__ __forceinline__ void combine_warps(const Shared<T, D, NT>& sh, int co
   for (int i = 0; i < kWarps; ++i) {
     const float f = ex2f(sh.m[i][col] - n_use);
     w = fmaf(f, sh.l[i][col], w);
-    acc = fmaf(f, sh.o[i][col][c], acc);
+    acc = fmaf(f, sh.out(i, col)[c], acc);
   }
 }
 
@@ -382,11 +581,17 @@ struct Queries {
       x[c] = r < n ? fresh(reinterpret_cast<const uint4*>(q + at)) : make_uint4(0u, 0u, 0u, 0u);
     }
   }
-  __device__ __forceinline__ void store(Shared<T, D, NT>& sh, int warp, int lane) const {
+  __device__ __forceinline__ void store(SharedOf<T, D, NT>& sh, int warp, int lane) const {
     if (warp >= NT) return;
 #pragma unroll
     for (int c = 0; c < kLoads; ++c) {
-      if constexpr (sizeof(T) == 2) {
+      if constexpr (kStaged<T, NT>) {  // columns as they are: 16 i + 2 j' and + 8 are what lane (x, j') has of step i
+        uint32_t* step = reinterpret_cast<uint32_t*>(sh.q[warp].step[4 * (c >> 1) + (lane & 3)]) + (lane >> 2) * 8 + (c & 1);
+        step[0] = x[c].x;
+        step[2] = x[c].y;
+        step[4] = x[c].z;
+        step[6] = x[c].w;
+      } else if constexpr (sizeof(T) == 2) {
         sh.q[warp].step[2 * c][lane] = make_uint2(x[c].x, x[c].y);
         sh.q[warp].step[2 * c + 1][lane] = make_uint2(x[c].z, x[c].w);
       } else {
@@ -406,7 +611,7 @@ template <typename T, int D, int NT>
 __device__ __forceinline__ Walk<T, D, NT> make_walk(const AttnParams& p, const DecodeArgs& a, int b, int row0, int n, int len, int item, int lane) {
   const int x = lane >> 2, j = lane & 3, g = item * a.Gi / p.G;
   Walk<T, D, NT> w{p, static_cast<const T*>(p.k) + (int64_t)g * p.ks.head + (sizeof(T) == 2 ? 16 : 8) * j,
-                   static_cast<const T*>(p.v) + (int64_t)g * p.vs.head + x * (D / 8), b, len, lane, p.scale * 1.4426950408889634f, {}};
+                   static_cast<const T*>(p.v) + (int64_t)g * p.vs.head + x * (D / 8), b, g, len, lane, p.scale * 1.4426950408889634f, {}};
 #pragma unroll
   for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
@@ -442,12 +647,15 @@ __device__ __forceinline__ void end(const AttnParams& p) {
 
 // ---- an item per cluster
 template <typename T, int D, int NT, int kAhead>
-__global__ void __launch_bounds__(kThreads, 1) paged_decode_cluster_kernel(const __grid_constant__ AttnParams p, const __grid_constant__ DecodeArgs a) {
+__global__ void __launch_bounds__(kThreads, 1) paged_decode_cluster_kernel(const __grid_constant__ AttnParams p, const __grid_constant__ DecodeArgs a,
+    const __grid_constant__ MapsOf<T, NT> maps) {
   extern __shared__ __align__(16) uint8_t smem[];
-  Shared<T, D, NT>& sh = *reinterpret_cast<Shared<T, D, NT>*>(smem);
+  SharedOf<T, D, NT>& sh = shared_of<T, D, NT>(smem);
   __shared__ float s_o[8 * NT * D + kClusterMost], s_n[kClusterMost][8 * NT], s_w[kClusterMost][8 * NT];  // from each CTA of the cluster
   const int rank = blockIdx.x, n_cta = a.n_cta, item = blockIdx.y, b = blockIdx.z;
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+  set_up<T, D, NT>(sh, warp, lane);
+  uint32_t used = 0;
   begin(p);
   asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");  // everyone has started: its shared memory may be written
   // everything that may be needed is asked for at once
@@ -468,11 +676,11 @@ __global__ void __launch_bounds__(kThreads, 1) paged_decode_cluster_kernel(const
   const Walk<T, D, NT> walk = make_walk<T, D, NT>(p, a, b, rows.x, rows.y, len, item, lane);
   State<D, NT> st;
   clear(st);
-  walk.template run<kAhead>(st, sh.q, first, stride, first < blocks ? (blocks - first + stride - 1) / stride : 0, [&]() {
+  walk.template run<kAhead>(st, sh, maps, used, warp, first, stride, first < blocks ? (blocks - first + stride - 1) / stride : 0, [&]() {
     queries.store(sh, warp, lane);
     __syncthreads();
   }, &early);
-  publish(sh, st, warp, lane);
+  publish<T, D, NT>(sh, st, warp, lane);
   asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
   __syncthreads();
   // CTA r finishes outputs r * per_cta ..; every CTA sends it its share of them
@@ -484,7 +692,7 @@ __global__ void __launch_bounds__(kThreads, 1) paged_decode_cluster_kernel(const
   };
   for (int i = tid; i < outputs; i += kThreads) {
     float n, w, acc;
-    combine_warps(sh, i / D, i % D, n, w, acc);
+    combine_warps<T, D, NT>(sh, i / D, i % D, n, w, acc);
     const int to = i / per_cta;
     send(&s_o[rank * per_cta + i - to * per_cta], to, acc);
     if (i % D < n_cta) {
@@ -493,7 +701,7 @@ __global__ void __launch_bounds__(kThreads, 1) paged_decode_cluster_kernel(const
     }
   }
   asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
-  const int here = min(per_cta, outputs - rank * per_cta);
+  const int here = gave_up<T, NT>(p) ? 0 : min(per_cta, outputs - rank * per_cta);
   for (int o = tid; o < here; o += kThreads) {
     const int col = (rank * per_cta + o) / D, c = (rank * per_cta + o) % D;
     float n = -INFINITY, w = 0.f, acc = 0.f;
@@ -583,10 +791,13 @@ __device__ __forceinline__ Share share_of(const AttnParams& p, const DecodeArgs&
 }
 
 template <typename T, int D, int NT, int kAhead>
-__global__ void __launch_bounds__(kThreads, 1) paged_decode_shares_kernel(const __grid_constant__ AttnParams p, const __grid_constant__ DecodeArgs a) {
+__global__ void __launch_bounds__(kThreads, 1) paged_decode_shares_kernel(const __grid_constant__ AttnParams p, const __grid_constant__ DecodeArgs a,
+    const __grid_constant__ MapsOf<T, NT> maps) {
   extern __shared__ __align__(16) uint8_t smem[];
-  Shared<T, D, NT>& sh = *reinterpret_cast<Shared<T, D, NT>*>(smem);
+  SharedOf<T, D, NT>& sh = shared_of<T, D, NT>(smem);
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, cta = blockIdx.x;
+  set_up<T, D, NT>(sh, warp, lane);
+  uint32_t used = 0;
   begin(p);
   if (warp == kWarps - 1) clear_empty<T, D>(p, cta, a.n_cta, lane);
   const Share r = share_of(p, a, cta, lane);
@@ -602,16 +813,17 @@ __global__ void __launch_bounds__(kThreads, 1) paged_decode_shares_kernel(const 
   State<D, NT> st;
   clear(st);
   const int blocks = (r.len + 15) / 16, last = (int)((int64_t)blocks * (r.part + 1) / r.parts), first = (int)((int64_t)blocks * r.part / r.parts) + warp;
-  walk.template run<kAhead>(st, sh.q, first, kWarps, first < last ? (last - first + kWarps - 1) / kWarps : 0, []() { __syncthreads(); });
-  publish(sh, st, warp, lane);
+  walk.template run<kAhead>(st, sh, maps, used, warp, first, kWarps, first < last ? (last - first + kWarps - 1) / kWarps : 0, []() { __syncthreads(); });
+  publish<T, D, NT>(sh, st, warp, lane);
   __syncthreads();
   float* part = a.partials + (int64_t)cta * (8 * NT * (D + 2));
+  const bool keep = !gave_up<T, NT>(p);
   for (int i = tid; i < r.rows * a.Gi * D; i += kThreads) {
     const int col = i / D, c = i % D;
     float n, w, acc;
-    combine_warps(sh, col, c, n, w, acc);
+    combine_warps<T, D, NT>(sh, col, c, n, w, acc);
     if (r.parts == 1) {
-      write_out<T>(p, a, r.row0, r.item, col, c, n, w, acc);
+      if (keep) write_out<T>(p, a, r.row0, r.item, col, c, n, w, acc);
     } else {
       part[i] = acc;
       if (c == 0) {
@@ -630,7 +842,7 @@ __global__ void __launch_bounds__(kJoinThreads) paged_decode_join_shares_kernel(
   grid_wait();
   const int4 j = __ldcg(a.joins + blockIdx.x);  // parts (0: none), first row, rows, item
   const int i = blockIdx.y * kJoinThreads + threadIdx.x;
-  if (i >= j.z * a.Gi * D || j.x == 0) return;
+  if (i >= j.z * a.Gi * D || j.x == 0 || gave_up<T, NT>(p)) return;
   const int col = i / D, c = i % D;
   auto part = [&](int k) { return a.partials + (int64_t)(blockIdx.x + k * a.items) * (8 * NT * (D + 2)); };
   float n = -INFINITY, w = 0.f, acc = 0.f;
@@ -649,13 +861,16 @@ __global__ void __launch_bounds__(kJoinThreads) paged_decode_join_shares_kernel(
 
 // ---- ranges of equal length
 template <typename T, int D, int NT, int kAhead>
-__global__ void __launch_bounds__(kThreads, sizeof(T) == 2 && D == 64 ? 2 : 1) paged_decode_ranges_kernel(const __grid_constant__ AttnParams p, const __grid_constant__ DecodeArgs a) {
+__global__ void __launch_bounds__(kThreads, sizeof(T) == 2 && D == 64 && !kStaged<T, NT> ? 2 : 1) paged_decode_ranges_kernel(const __grid_constant__ AttnParams p, const __grid_constant__ DecodeArgs a,
+    const __grid_constant__ MapsOf<T, NT> maps) {
   extern __shared__ __align__(16) uint8_t smem[];
-  Shared<T, D, NT>& sh = *reinterpret_cast<Shared<T, D, NT>*>(smem);
+  SharedOf<T, D, NT>& sh = shared_of<T, D, NT>(smem);
   __shared__ int s_group[kMaxGroups + 1];  // blocks (of one item) of the groups of 32 sequences before
   __shared__ RangeStart s_start;
   const PagedDev& g = p.paged;
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, cta = blockIdx.x;
+  set_up<T, D, NT>(sh, warp, lane);
+  uint32_t used = 0;
   begin(p);
   if (warp == kWarps - 1) clear_empty<T, D>(p, cta, a.n_cta, lane);
   const int groups = (g.batch + 31) / 32;
@@ -737,17 +952,18 @@ __global__ void __launch_bounds__(kThreads, sizeof(T) == 2 && D == 64 ? 2 : 1) p
     State<D, NT> st;
     clear(st);
     const int first = s0 + warp;
-    walk.template run<kAhead>(st, sh.q, first, kWarps, first < s1 ? (s1 - first + kWarps - 1) / kWarps : 0, []() { __syncthreads(); });
-    publish(sh, st, warp, lane);
+    walk.template run<kAhead>(st, sh, maps, used, warp, first, kWarps, first < s1 ? (s1 - first + kWarps - 1) / kWarps : 0, []() { __syncthreads(); });
+    publish<T, D, NT>(sh, st, warp, lane);
     __syncthreads();
     const bool whole = s0 == 0 && s1 == blocks;
     float* part = a.partials + (int64_t)(cta * 2 + (s0 > 0 ? 0 : 1)) * (8 * NT * (D + 2));
+    const bool keep = !gave_up<T, NT>(p);
     for (int i = tid; i < cols * D; i += kThreads) {
       const int col = i / D, c = i % D;
       float n, w, acc;
-      combine_warps(sh, col, c, n, w, acc);
+      combine_warps<T, D, NT>(sh, col, c, n, w, acc);
       if (whole) {
-        write_out<T>(p, a, rows.x, item, col, c, n, w, acc);
+        if (keep) write_out<T>(p, a, rows.x, item, col, c, n, w, acc);
       } else {
         part[i] = acc;
         if (c == 0) {
@@ -765,6 +981,8 @@ __global__ void __launch_bounds__(kThreads, sizeof(T) == 2 && D == 64 ? 2 : 1) p
       if (b >= g.batch) break;
     }
     __syncthreads();  // the shares and queries have been read
+    if constexpr (kStaged<T, NT>)
+      if (sh.words[1]) break;  // (of this CTA's waits, so the same for all of it)
   }
   end(p);
 }
@@ -776,7 +994,7 @@ __global__ void __launch_bounds__(kThreads) paged_decode_join_kernel(const __gri
   grid_wait();
   const int at = blockIdx.x + 1;
   const RangeStart r = a.starts[at];
-  if (r.b < 0 || r.before == 0) return;
+  if (r.b < 0 || r.before == 0 || gave_up<T, NT>(p)) return;
   const int n_ranges = ranges_of(r.total, a.n_cta);
   auto start = [&](int i) { return r.total * i / n_ranges; };
   const int64_t u0 = start(at) - r.before, u1 = u0 + r.blocks;  // the item
@@ -804,6 +1022,10 @@ __global__ void __launch_bounds__(kThreads) paged_decode_join_kernel(const __gri
 template <typename F>
 cudaError_t with_shape(cascade_dtype_t dtype, int d, int columns, F f) {
   auto with_columns = [&](auto t, auto dim) {
+    if constexpr (sizeof(t) == 2) {
+      if (columns > 24) return f(t, dim, std::integral_constant<int, 4>());
+      if (columns > 16) return f(t, dim, std::integral_constant<int, 3>());
+    }
     return columns <= 8 ? f(t, dim, std::integral_constant<int, 1>()) : f(t, dim, std::integral_constant<int, 2>());
   };
   auto with_dim = [&](auto t) {
@@ -812,50 +1034,84 @@ cudaError_t with_shape(cascade_dtype_t dtype, int d, int columns, F f) {
   return dtype == CASCADE_BF16 ? with_dim(__nv_bfloat16()) : with_dim(float());
 }
 
-int ranges_cta(cascade_dtype_t dtype, int d) { return d == 128 || dtype == CASCADE_F32 ? 148 : 296; }  // CTAs that are resident at a time
-int64_t decode_items(const AttnParams& p) { return (int64_t)p.paged.batch * (p.H / paged_decode_heads(p)); }
+// CTAs that are resident at a time
+int ranges_cta(cascade_dtype_t dtype, int d, int columns) { return d == 128 || dtype == CASCADE_F32 || columns > kMostInRegisters ? 148 : 296; }
+int columns_most(cascade_dtype_t dtype) { return dtype == CASCADE_BF16 ? kMostColumns : 16; }
 // Clusters only where all of them are resident at once with a CTA per SM (of 16, 10, 8, 4, 2 CTAs 7, 11, 15, 33, 74 are), and, with more
 // than one sequence, only over short caches: it is not known here how long they are, and one long sequence would be left to its clusters.
 // us, caches new to L2, 32 / 8 heads of 128 (clusters | shares | ranges, 6 us of them the events'): 4 sequences of 2500 rows 20 | 24 | 33,
 // of 8000 35 | 39 | 48, 6 of 1000 to 8000 52 | 40 | 45, of 30000 163 | 132 | 140, 16 of 300 17 | 20 | 26, of 1000 to 8000 92 | 94 | 75.
-int cluster_size(const AttnParams& p) {  // 0: shares or ranges
-  const int64_t items = decode_items(p), blocks = ((int64_t)p.paged.max_pages * p.paged.page_size + 15) / 16;
+// And a CTA an item, in turns, where no sequence can be long: the ranges pay for every item that they cross, and for the second kernel.
+// us, the same heads (CTAs | ranges): 32 sequences of 100 to 300 rows 14 | 24, 64 of 500 to 1000 51 | 57, 24 of 250 to 2000 37 | 44 but of
+// 1500 to 2000 48 | 45; drafts of 2 to 6 rows, 32 of 100 to 300 27 | 41, 64 of 1500 to 2000 109 | 114, 24 of 500 to 4000 72 | 74; fp32,
+// 64 of 40 to 160 31 | 48, of 900 to 1000 116 | 110.
+int cluster_size(const AttnParams& p, cascade_dtype_t dtype, int64_t items, int columns) {  // 0: shares or ranges
+  const int64_t blocks = ((int64_t)p.paged.max_pages * p.paged.page_size + 15) / 16;
   int n = 0;
   for (const auto& fit : {std::pair<int, int>{148, 1}, {74, 2}, {33, 4}, {15, 8}, {11, 10}, {7, 16}})
     if (items <= fit.first) n = fit.second;
-  if (n == 0) return 0;
+  if (n == 0) return blocks <= (columns > 8 ? 16 : 8) * kWarps / (dtype == CASCADE_F32 ? 2 : 1) ? 1 : 0;
   n = (int)std::min<int64_t>(n, (blocks + kWarps - 1) / kWarps);
   return p.paged.batch == 1 || blocks <= 10 * kWarps * n ? n : 0;
 }
-bool shares(const AttnParams& p) { return decode_items(p) <= 74; }  // two CTAs an item
+bool shares(int64_t items) { return items <= 74; }  // two CTAs an item
+
+bool encode_blocks(CUtensorMap* map, const void* base, const Strides& st, const AttnParams& p) {
+  EncodeTiledFn fn = encode_tiled_fn();
+  if (!fn) return false;
+  const PagedDev& g = p.paged;
+  const cuuint64_t dims[5] = {64, (cuuint64_t)g.page_size, (cuuint64_t)p.d / 64, (cuuint64_t)p.Hkv, (cuuint64_t)g.n_pages};
+  auto stride = [&](int64_t elems, int64_t extent) { return (cuuint64_t)(extent > 1 ? elems * 2 : p.d * 2); };
+  const cuuint64_t strides[4] = {stride(st.token, g.page_size), 128, stride(st.head, p.Hkv), stride(st.batch, g.n_pages)};
+  const cuuint32_t box[5] = {64, 16, (cuuint32_t)p.d / 64, 1, 1}, one[5] = {1, 1, 1, 1, 1};
+  return fn(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 5, const_cast<void*>(base), dims, strides, box, one, CU_TENSOR_MAP_INTERLEAVE_NONE,
+            CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
 
 }  // namespace
 
-// Heads of an item: the largest divisor of the group that fits the columns.
-int paged_decode_heads(const AttnParams& p) {
+// Heads of an item of `rows` rows: the largest divisor of the group that fits the columns.
+int paged_decode_heads(const AttnParams& p, cascade_dtype_t dtype, int rows) {
   for (int n = std::min(16, p.G); n > 1; --n)
-    if (p.G % n == 0) return n;
+    if (p.G % n == 0 && rows * n <= columns_most(dtype)) return n;
   return 1;
 }
-int paged_decode_rows(const AttnParams& p) { return 16 / paged_decode_heads(p); }
+int paged_decode_rows(const AttnParams& p, cascade_dtype_t dtype) { return columns_most(dtype) / paged_decode_heads(p, dtype, 1); }
+
+// More columns than that in two items or more, where the items are few: the rows of the cache are read by each (from L2 by all but one),
+// and the products are as slow as they are.  us, 64 / 8 heads of 128 over 3000 to 9000 rows (split | tiles): 2 sequences of 8 rows
+// 35 | 46, 4 of 6 55 | 51, 4 of 8 65 | 48; 8 / 1 heads, 16 of 2 to 6 rows 28 | 44.
+bool paged_decode_splits(const AttnParams& p, cascade_dtype_t dtype, int rows) {
+  return dtype == CASCADE_BF16 && rows <= 8 && (int64_t)p.paged.batch * (p.H / paged_decode_heads(p, dtype, rows)) <= 37;
+}
 
 size_t paged_decode_ws_bytes(const AttnParams& p, cascade_dtype_t dtype, int rows) {
-  if (cluster_size(p) > 0) return 0;
-  const int columns = rows * paged_decode_heads(p) <= 8 ? 8 : 16, n = ranges_cta(dtype, p.d);
-  if (shares(p)) return (size_t)n * (columns * (p.d + 2) * 4 + sizeof(int4));
+  const int heads = paged_decode_heads(p, dtype, rows);
+  const int64_t items = (int64_t)p.paged.batch * (p.H / heads);
+  const int columns = (rows * heads + 7) / 8 * 8, n = ranges_cta(dtype, p.d, columns);
+  if (cluster_size(p, dtype, items, columns) > 0) return 0;
+  if (shares(items)) return (size_t)n * (columns * (p.d + 2) * 4 + sizeof(int4));
   return (size_t)n * (2 * columns * (p.d + 2) * 4 + sizeof(RangeStart));
 }
 
 cudaError_t launch_paged_decode(const AttnParams& p, cascade_dtype_t dtype, int rows, void* workspace, cudaStream_t stream) {
   DecodeArgs a = {};
-  a.Gi = paged_decode_heads(p);
+  a.Gi = paged_decode_heads(p, dtype, rows);
   a.items = p.H / a.Gi;
-  const int columns = rows * a.Gi, cluster = cluster_size(p);
+  const int64_t items = (int64_t)p.paged.batch * a.items;
+  const int columns = rows * a.Gi, cluster = cluster_size(p, dtype, items, columns);
   TimedLaunch timed(stream);
   return with_shape(dtype, p.d, columns, [&](auto t, auto d, auto nt) {
     using T = decltype(t);
     constexpr int D = decltype(d)::value, NT = decltype(nt)::value;
-    constexpr int smem = (int)sizeof(Shared<T, D, NT>);
+    constexpr int smem = kSmemBytes<T, D, NT>;
+    MapsOf<T, NT> maps;
+    if constexpr (kStaged<T, NT>) {
+      if (!encode_blocks(&maps.k, p.k, p.ks, p) || !encode_blocks(&maps.v, p.v, p.vs, p)) {
+        set_error("cascade_attn_paged: could not build the TMA descriptors of the pages");
+        return cudaErrorInvalidValue;
+      }
+    }
     // Blocks ahead: as many as an SM has registers for.  bf16, heads of 128: two and a CTA per SM (one ahead and two CTAs keep as
     // many loads in flight, but the walk spills: 64 sequences of up to 16384 rows 466 us, 385 this way).
     if (cluster > 0) {
@@ -865,9 +1121,9 @@ cudaError_t launch_paged_decode(const AttnParams& p, cascade_dtype_t dtype, int 
       if (e == cudaSuccess && cluster > 8) e = cudaFuncSetAttribute(kernel, cudaFuncAttributeNonPortableClusterSizeAllowed, 1);
       if (e != cudaSuccess) return e;
       a.n_cta = cluster;
-      return launch_dependent(kernel, dim3(cluster, a.items, p.paged.batch), kThreads, smem, cluster, true, stream, p, a);
+      return launch_dependent(kernel, dim3(cluster, a.items, p.paged.batch), kThreads, smem, cluster, true, stream, p, a, maps);
     }
-    if (shares(p)) {
+    if (shares(items)) {
       constexpr int kAhead = sizeof(T) == 4 && D == 128 ? 1 : 2;
       a.n_cta = 148;
       a.joins = static_cast<int4*>(workspace);
@@ -875,18 +1131,18 @@ cudaError_t launch_paged_decode(const AttnParams& p, cascade_dtype_t dtype, int 
       auto kernel = paged_decode_shares_kernel<T, D, NT, kAhead>;
       cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
       if (e != cudaSuccess) return e;
-      e = launch_dependent(kernel, dim3(a.n_cta), kThreads, smem, 1, true, stream, p, a);
+      e = launch_dependent(kernel, dim3(a.n_cta), kThreads, smem, 1, true, stream, p, a, maps);
       if (e != cudaSuccess) return e;
       return launch_dependent(paged_decode_join_shares_kernel<T, D, NT>, dim3(a.n_cta, (rows * a.Gi * D + kJoinThreads - 1) / kJoinThreads), kJoinThreads, 0, 1, true, stream, p, a);
     }
     constexpr int kAhead = sizeof(T) == 2 ? (D == 128 && NT == 1 ? 2 : 1) : (D == 64 && NT == 1 ? 2 : 1);
-    a.n_cta = ranges_cta(dtype, p.d);
+    a.n_cta = ranges_cta(dtype, p.d, columns);
     a.starts = static_cast<RangeStart*>(workspace);
     a.partials = reinterpret_cast<float*>(a.starts + a.n_cta);
     auto kernel = paged_decode_ranges_kernel<T, D, NT, kAhead>;
     cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
     if (e != cudaSuccess) return e;
-    e = launch_dependent(kernel, dim3(a.n_cta), kThreads, smem, 1, true, stream, p, a);
+    e = launch_dependent(kernel, dim3(a.n_cta), kThreads, smem, 1, true, stream, p, a, maps);
     if (e != cudaSuccess) return e;
     return launch_dependent(paged_decode_join_kernel<T, D, NT>, dim3(a.n_cta - 1), kThreads, 0, 1, true, stream, p, a);
   });

@@ -117,6 +117,28 @@ def test_logits_of_minus_infinity_and_the_lowest_value():
         assert (out[:news[0]].double().cpu() - o_ref[:news[0]]).abs().max() < 0.03 and (lse[:news[0]].double().cpu() - lse_ref[:news[0]]).abs().max() < 1e-3
 
 
+@pytest.mark.parametrize("d", [128, 64])
+@pytest.mark.parametrize("H,Hkv", [(1, 1), (12, 12), (4, 2), (6, 2), (8, 2), (14, 2), (8, 1), (24, 2), (32, 2)])
+@pytest.mark.parametrize("n", [1, 2, 5, 60])
+def test_drafts_of_every_width(d, H, Hkv, n):
+    """Up to 32 (row, head) pairs of a KV head, and one row more: one sequence, a few over short and over wide tables, many; lengths that
+    end inside a block of 16 and inside a page, and caches shorter than the drafts."""
+    group, rng = H // Hkv, np.random.default_rng(100 * n + H)
+    for pairs in (9, 16, 17, 24, 25, 32):
+        rows = max(1, min(pairs, 32) // group)
+        news = [rows] + [int(x) for x in rng.integers(0, rows + 1, n - 1)]
+        lens = [int(x) for x in rng.integers(0, 500, n)]
+        lens[0], lens[-1] = 16 * 23 + 1 + pairs % 16, max(1, rows - 1)
+        strided = pairs == 16
+        for width in ([0, 2000] if n > 1 else [0]):
+            b = pu.Batch(news, lens, H, Hkv, d, 48 if pairs == 24 else 16 if pairs == 32 else 64, seed=pairs, head_major=pairs == 25, strided=strided,
+                         **({"width": width} if width else {}))
+            attend(b, max_rows=rows)
+            if width == 0 and pairs in (17, 32):
+                attend(b, causal=False, max_rows=rows + 1)
+                attend(b, visible=rng.integers(-3, 600, b.n), max_rows=rows)
+
+
 def test_long_cache_and_many_sequences():
     attend(pu.Batch([1, 4], [20001, 9000], 8, 2, 128, 64, seed=1), max_rows=4)
     attend(pu.Batch([1] * 300, [1 + 7 * i % 200 for i in range(300)], 4, 2, 64, 16, seed=2), max_rows=1)
