@@ -38,6 +38,7 @@ namespace cascade {
 namespace {
 
 constexpr int kWarps = 8, kThreads = kWarps * 32, kJoinThreads = 128;
+constexpr int kRangeWarps = 4, kRangeThreads = kRangeWarps * 32;  // of a CTA that walks ranges
 constexpr int kMaxGroups = 2048;  // groups of 32 sequences
 constexpr int kClusterMost = 16;
 constexpr int kMostInRegisters = 8, kMostColumns = 32;
@@ -63,7 +64,7 @@ __device__ __forceinline__ int blocks_of(const PagedDev& g, int b) {
   return (paged_len(g, b) + 15) / 16;
 }
 __device__ __forceinline__ int ranges_of(int64_t total, int n_cta) {  // a block for every warp at least
-  return (int)max((int64_t)1, min((int64_t)n_cta, (total + kWarps - 1) / kWarps));
+  return (int)max((int64_t)1, min((int64_t)n_cta, (total + kRangeWarps - 1) / kRangeWarps));
 }
 
 // Query fragments: B operand of a k-step, lane (column, j); fp32: the upper parts of both values, then the rests
@@ -87,29 +88,29 @@ constexpr int kStages = 384 / D;  // blocks of a warp's ring, 24 KiB
 template <int D>
 constexpr int kPartBytes = 16 * D * 2;  // keys or values of a block: boxes of 16 rows and 64 columns, 128-byte swizzle
 
-template <typename T, int D, int NT, bool kStaged>
+template <typename T, int D, int NT, int W, bool kStaged>
 struct Shared {
-  float o[kWarps][8 * NT][D + 4];
-  float m[kWarps][8 * NT], l[kWarps][8 * NT];
+  float o[W][8 * NT][D + 4];
+  float m[W][8 * NT], l[W][8 * NT];
   Fragments<T, D> q[NT];
   __device__ __forceinline__ float* out(int warp, int col) { return o[warp][col]; }
   __device__ __forceinline__ const float* out(int warp, int col) const { return o[warp][col]; }
 };
-template <typename T, int D, int NT>
-struct Shared<T, D, NT, true> {
-  uint8_t ring[kWarps][kStages<D>][2][kPartBytes<D>];  // and a warp's outputs, once it has walked all its blocks
-  float m[kWarps][8 * NT], l[kWarps][8 * NT];
+template <typename T, int D, int NT, int W>
+struct Shared<T, D, NT, W, true> {
+  uint8_t ring[W][kStages<D>][2][kPartBytes<D>];  // and a warp's outputs, once it has walked all its blocks
+  float m[W][8 * NT], l[W][8 * NT];
   Fragments<T, D> q[NT];
-  uint64_t full[kWarps][kStages<D>];
-  int words[2 + kWarps];  // WaitCtx
+  uint64_t full[W][kStages<D>];
+  int words[2 + W];  // WaitCtx
   static_assert(8 * NT * (D + 4) * 4 <= kStages<D> * 2 * kPartBytes<D>, "a warp's outputs lie in its ring");
   __device__ __forceinline__ float* out(int warp, int col) { return reinterpret_cast<float*>(ring[warp][0][0]) + col * (D + 4); }
   __device__ __forceinline__ const float* out(int warp, int col) const { return reinterpret_cast<const float*>(ring[warp][0][0]) + col * (D + 4); }
 };
-template <typename T, int D, int NT>
-using SharedOf = Shared<T, D, NT, kStaged<T, NT>>;
-template <typename T, int D, int NT>
-constexpr int kSmemBytes = (int)sizeof(SharedOf<T, D, NT>) + (kStaged<T, NT> ? 1024 : 0);  // the ring starts at a multiple of 1024
+template <typename T, int D, int NT, int W>
+using SharedOf = Shared<T, D, NT, W, kStaged<T, NT>>;
+template <typename T, int D, int NT, int W>
+constexpr int kSmemBytes = (int)sizeof(SharedOf<T, D, NT, W>) + (kStaged<T, NT> ? 1024 : 0);  // the ring starts at a multiple of 1024
 
 struct alignas(64) PageMaps {
   CUtensorMap k, v;  // [page][head][64-column half][row of the page][64 columns]
@@ -118,16 +119,16 @@ struct NoMaps {};
 template <typename T, int NT>
 using MapsOf = std::conditional_t<kStaged<T, NT>, PageMaps, NoMaps>;
 
-template <typename T, int D, int NT>
-__device__ __forceinline__ SharedOf<T, D, NT>& shared_of(uint8_t* smem) {
+template <typename T, int D, int NT, int W>
+__device__ __forceinline__ SharedOf<T, D, NT, W>& shared_of(uint8_t* smem) {
   if constexpr (kStaged<T, NT>) smem += (0u - tc::smem_u32(smem)) & 1023u;
-  return *reinterpret_cast<SharedOf<T, D, NT>*>(smem);
+  return *reinterpret_cast<SharedOf<T, D, NT, W>*>(smem);
 }
 // (every warp its own barriers; the words are there after the next __syncthreads)
-template <typename T, int D, int NT>
-__device__ __forceinline__ void set_up(SharedOf<T, D, NT>& sh, int warp, int lane) {
+template <typename T, int D, int NT, int W>
+__device__ __forceinline__ void set_up(SharedOf<T, D, NT, W>& sh, int warp, int lane) {
   if constexpr (kStaged<T, NT>) {
-    if (warp == 0 && lane < 2 + kWarps) sh.words[lane] = 0;
+    if (warp == 0 && lane < 2 + W) sh.words[lane] = 0;
     if (lane == 0)
       for (int i = 0; i < kStages<D>; ++i) tc::mbar_init(tc::smem_u32(&sh.full[warp][i]), 1);
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
@@ -355,11 +356,11 @@ struct Walk {
     }
   }
   // The same walk over rows that TMA brings.  `used`: blocks that the warp's ring has had.
-  template <typename Shared, typename Ready>
-  __device__ __forceinline__ void run_staged(State<D, NT>& st, Shared& sh, const PageMaps& maps, uint32_t& used, int warp, int first, int stride,
+  template <int W, typename Ready>
+  __device__ __forceinline__ void run_staged(State<D, NT>& st, SharedOf<T, D, NT, W>& sh, const PageMaps& maps, uint32_t& used, int warp, int first, int stride,
                                              int count, Ready ready, const int* early = nullptr) const {
     constexpr int S = kStages<D>;
-    const tc::WaitCtx<false, kWarps> wc{tc::smem_u32(sh.words), p.paged.status};
+    const tc::WaitCtx<false, W> wc{tc::smem_u32(sh.words), p.paged.status};
     int pages = lane >= count ? 0 : early ? paged_checked(p.paged, b, *early) : page_of(first + lane * stride), pages_next = 0;
     auto page_at = [&](int t) {  // (asked in order)
       if ((t & 31) == 0 && t > 0) pages = pages_next;
@@ -445,10 +446,10 @@ struct Walk {
   }
 
   // blocks first, first + stride, .. (count of them)
-  template <int kAhead, typename Ready>
-  __device__ __forceinline__ void run(State<D, NT>& st, SharedOf<T, D, NT>& sh, const MapsOf<T, NT>& maps, uint32_t& used, int warp, int first,
+  template <int kAhead, int W, typename Ready>
+  __device__ __forceinline__ void run(State<D, NT>& st, SharedOf<T, D, NT, W>& sh, const MapsOf<T, NT>& maps, uint32_t& used, int warp, int first,
                                       int stride, int count, Ready ready, const int* early = nullptr) const {
-    if constexpr (kStaged<T, NT>) run_staged(st, sh, maps, used, warp, first, stride, count, ready, early);
+    if constexpr (kStaged<T, NT>) run_staged<W>(st, sh, maps, used, warp, first, stride, count, ready, early);
     else run_registers<kAhead>(st, sh.q, first, stride, count, ready, early);
   }
   template <int kAhead, typename Ready>
@@ -512,8 +513,8 @@ struct Walk {
   }
 };
 
-template <typename T, int D, int NT>
-__device__ __forceinline__ void publish(SharedOf<T, D, NT>& sh, const State<D, NT>& st, int warp, int lane) {
+template <typename T, int D, int NT, int W>
+__device__ __forceinline__ void publish(SharedOf<T, D, NT, W>& sh, const State<D, NT>& st, int warp, int lane) {
   const int x = lane >> 2, j = lane & 3;
 #pragma unroll
   for (int nt = 0; nt < NT; ++nt)
@@ -539,27 +540,59 @@ __device__ __forceinline__ void publish(SharedOf<T, D, NT>& sh, const State<D, N
       }
     }
 }
-// Output column c of column `col`: maximum, sum of weights and weighted sum over the warps
-template <typename T, int D, int NT>
-__device__ __forceinline__ void combine_warps(const SharedOf<T, D, NT>& sh, int col, int c, float& n, float& w, float& acc) {
+// Output columns c .. c + 3 of column `col`: maximum, sum of weights and weighted sums over the warps
+__device__ __forceinline__ void add4(float4& acc, float f, const float4& v) {
+  acc = make_float4(fmaf(f, v.x, acc.x), fmaf(f, v.y, acc.y), fmaf(f, v.z, acc.z), fmaf(f, v.w, acc.w));
+}
+template <typename T, int D, int NT, int W>
+__device__ __forceinline__ void combine_warps(const SharedOf<T, D, NT, W>& sh, int col, int c, float& n, float& w, float4& acc) {
   n = -INFINITY;
 #pragma unroll
-  for (int i = 0; i < kWarps; ++i) n = fmaxf(n, sh.m[i][col]);
+  for (int i = 0; i < W; ++i) n = fmaxf(n, sh.m[i][col]);
   const float n_use = n == -INFINITY ? 0.f : n;
-  w = acc = 0.f;
+  w = 0.f;
+  acc = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll
-  for (int i = 0; i < kWarps; ++i) {
+  for (int i = 0; i < W; ++i) {
     const float f = ex2f(sh.m[i][col] - n_use);
     w = fmaf(f, sh.l[i][col], w);
-    acc = fmaf(f, sh.out(i, col)[c], acc);
+    add4(acc, f, *reinterpret_cast<const float4*>(sh.out(i, col) + c));
+  }
+}
+// The same over the partials of an item: part(k) for k < n_parts, each [columns][D], then the maxima, then the sums
+template <int D, int NT, typename Part>
+__device__ __forceinline__ void combine_parts(int n_parts, Part part, int col, int i, float& n, float& w, float4& acc) {
+  n = -INFINITY;
+#pragma unroll 4
+  for (int k = 0; k < n_parts; ++k) n = fmaxf(n, __ldcg(part(k) + 8 * NT * D + col));
+  const float n_use = n == -INFINITY ? 0.f : n;
+  w = 0.f;
+  acc = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll 4
+  for (int k = 0; k < n_parts; ++k) {
+    const float* q = part(k);
+    const float f = ex2f(__ldcg(q + 8 * NT * D + col) - n_use);
+    w = fmaf(f, __ldcg(q + 8 * NT * (D + 1) + col), w);
+    add4(acc, f, __ldcg(reinterpret_cast<const float4*>(q + i)));
+  }
+}
+template <int D, int NT>
+__device__ __forceinline__ void store_part(float* part, int col, int c, float n, float w, const float4& acc) {
+  *reinterpret_cast<float4*>(part + col * D + c) = acc;
+  if (c == 0) {
+    part[8 * NT * D + col] = n;
+    part[8 * NT * (D + 1) + col] = w;
   }
 }
 
-// Output column c of (row, head) of column `col`: n and w in log2 units
+// Output columns c .. c + 3 of (row, head) of column `col`: n and w in log2 units
 template <typename T>
-__device__ __forceinline__ void write_out(const AttnParams& p, const DecodeArgs& a, int row0, int item, int col, int c, float n, float w, float acc) {
+__device__ __forceinline__ void write_out(const AttnParams& p, const DecodeArgs& a, int row0, int item, int col, int c, float n, float w, const float4& acc) {
   const int r = col / a.Gi, row = row0 + r, head = item * a.Gi + col - r * a.Gi;
-  static_cast<T*>(p.o_out)[(int64_t)row * p.os.token + (int64_t)head * p.os.head + c] = static_cast<T>(w > 0.f ? acc / w : 0.f);
+  T* o = static_cast<T*>(p.o_out) + (int64_t)row * p.os.token + (int64_t)head * p.os.head + c;
+  const float4 v = w > 0.f ? make_float4(acc.x / w, acc.y / w, acc.z / w, acc.w / w) : make_float4(0.f, 0.f, 0.f, 0.f);
+  if constexpr (sizeof(T) == 2) *reinterpret_cast<uint2*>(o) = make_uint2(pack2_bf16(v.x, v.y), pack2_bf16(v.z, v.w));
+  else *reinterpret_cast<float4*>(o) = v;
   if (c == 0 && p.lse_out) p.lse_out[(int64_t)row * p.H + head] = w > 0.f ? n * 0.6931471805599453f + logf(w) : -INFINITY;
 }
 
@@ -581,7 +614,8 @@ struct Queries {
       x[c] = r < n ? fresh(reinterpret_cast<const uint4*>(q + at)) : make_uint4(0u, 0u, 0u, 0u);
     }
   }
-  __device__ __forceinline__ void store(SharedOf<T, D, NT>& sh, int warp, int lane) const {
+  template <typename Sh>
+  __device__ __forceinline__ void store(Sh& sh, int warp, int lane) const {
     if (warp >= NT) return;
 #pragma unroll
     for (int c = 0; c < kLoads; ++c) {
@@ -650,11 +684,12 @@ template <typename T, int D, int NT, int kAhead>
 __global__ void __launch_bounds__(kThreads, 1) paged_decode_cluster_kernel(const __grid_constant__ AttnParams p, const __grid_constant__ DecodeArgs a,
     const __grid_constant__ MapsOf<T, NT> maps) {
   extern __shared__ __align__(16) uint8_t smem[];
-  SharedOf<T, D, NT>& sh = shared_of<T, D, NT>(smem);
-  __shared__ float s_o[8 * NT * D + kClusterMost], s_n[kClusterMost][8 * NT], s_w[kClusterMost][8 * NT];  // from each CTA of the cluster
+  SharedOf<T, D, NT, kWarps>& sh = shared_of<T, D, NT, kWarps>(smem);
+  __shared__ __align__(16) float s_o[8 * NT * D + 4 * kClusterMost];
+  __shared__ float s_n[kClusterMost][8 * NT], s_w[kClusterMost][8 * NT];  // from each CTA of the cluster
   const int rank = blockIdx.x, n_cta = a.n_cta, item = blockIdx.y, b = blockIdx.z;
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-  set_up<T, D, NT>(sh, warp, lane);
+  set_up<T, D, NT, kWarps>(sh, warp, lane);
   uint32_t used = 0;
   begin(p);
   asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");  // everyone has started: its shared memory may be written
@@ -676,42 +711,46 @@ __global__ void __launch_bounds__(kThreads, 1) paged_decode_cluster_kernel(const
   const Walk<T, D, NT> walk = make_walk<T, D, NT>(p, a, b, rows.x, rows.y, len, item, lane);
   State<D, NT> st;
   clear(st);
-  walk.template run<kAhead>(st, sh, maps, used, warp, first, stride, first < blocks ? (blocks - first + stride - 1) / stride : 0, [&]() {
+  walk.template run<kAhead, kWarps>(st, sh, maps, used, warp, first, stride, first < blocks ? (blocks - first + stride - 1) / stride : 0, [&]() {
     queries.store(sh, warp, lane);
     __syncthreads();
   }, &early);
-  publish<T, D, NT>(sh, st, warp, lane);
+  publish<T, D, NT, kWarps>(sh, st, warp, lane);
   asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
   __syncthreads();
   // CTA r finishes outputs r * per_cta ..; every CTA sends it its share of them
-  const int outputs = cols * D, per_cta = (outputs + n_cta - 1) / n_cta;
-  auto send = [&](const float* local, int to, float v) {
+  const int outputs = cols * D, per_cta = ((outputs + n_cta - 1) / n_cta + 3) & ~3;
+  auto there = [&](const float* local, int to) {
     uint32_t addr;
     asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(addr) : "r"((uint32_t)__cvta_generic_to_shared(local)), "r"(to));
-    asm volatile("st.shared::cluster.f32 [%0], %1;" ::"r"(addr), "f"(v) : "memory");
+    return addr;
   };
-  for (int i = tid; i < outputs; i += kThreads) {
-    float n, w, acc;
-    combine_warps<T, D, NT>(sh, i / D, i % D, n, w, acc);
+  for (int i = 4 * tid; i < outputs; i += 4 * kThreads) {
+    float n, w;
+    float4 acc;
+    combine_warps<T, D, NT, kWarps>(sh, i / D, i % D, n, w, acc);
     const int to = i / per_cta;
-    send(&s_o[rank * per_cta + i - to * per_cta], to, acc);
-    if (i % D < n_cta) {
-      send(&s_n[rank][i / D], i % D, n);
-      send(&s_w[rank][i / D], i % D, w);
+    asm volatile("st.shared::cluster.v4.f32 [%0], {%1, %2, %3, %4};" ::"r"(there(&s_o[rank * per_cta + i - to * per_cta], to)), "f"(acc.x), "f"(acc.y), "f"(acc.z),
+                 "f"(acc.w)
+                 : "memory");
+    for (int c = i % D; c < min(i % D + 4, n_cta); ++c) {
+      asm volatile("st.shared::cluster.f32 [%0], %1;" ::"r"(there(&s_n[rank][i / D], c)), "f"(n) : "memory");
+      asm volatile("st.shared::cluster.f32 [%0], %1;" ::"r"(there(&s_w[rank][i / D], c)), "f"(w) : "memory");
     }
   }
   asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
   const int here = gave_up<T, NT>(p) ? 0 : min(per_cta, outputs - rank * per_cta);
-  for (int o = tid; o < here; o += kThreads) {
+  for (int o = 4 * tid; o < here; o += 4 * kThreads) {
     const int col = (rank * per_cta + o) / D, c = (rank * per_cta + o) % D;
-    float n = -INFINITY, w = 0.f, acc = 0.f;
+    float n = -INFINITY, w = 0.f;
+    float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
     for (int r = 0; r < n_cta; ++r) n = fmaxf(n, s_n[r][col]);
     const float n_use = n == -INFINITY ? 0.f : n;
 #pragma unroll 4
     for (int r = 0; r < n_cta; ++r) {
       const float f = ex2f(s_n[r][col] - n_use);
       w = fmaf(f, s_w[r][col], w);
-      acc = fmaf(f, s_o[r * per_cta + o], acc);
+      add4(acc, f, *reinterpret_cast<const float4*>(&s_o[r * per_cta + o]));
     }
     write_out<T>(p, a, rows.x, item, col, c, n, w, acc);
   }
@@ -794,9 +833,9 @@ template <typename T, int D, int NT, int kAhead>
 __global__ void __launch_bounds__(kThreads, 1) paged_decode_shares_kernel(const __grid_constant__ AttnParams p, const __grid_constant__ DecodeArgs a,
     const __grid_constant__ MapsOf<T, NT> maps) {
   extern __shared__ __align__(16) uint8_t smem[];
-  SharedOf<T, D, NT>& sh = shared_of<T, D, NT>(smem);
+  SharedOf<T, D, NT, kWarps>& sh = shared_of<T, D, NT, kWarps>(smem);
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, cta = blockIdx.x;
-  set_up<T, D, NT>(sh, warp, lane);
+  set_up<T, D, NT, kWarps>(sh, warp, lane);
   uint32_t used = 0;
   begin(p);
   if (warp == kWarps - 1) clear_empty<T, D>(p, cta, a.n_cta, lane);
@@ -813,24 +852,18 @@ __global__ void __launch_bounds__(kThreads, 1) paged_decode_shares_kernel(const 
   State<D, NT> st;
   clear(st);
   const int blocks = (r.len + 15) / 16, last = (int)((int64_t)blocks * (r.part + 1) / r.parts), first = (int)((int64_t)blocks * r.part / r.parts) + warp;
-  walk.template run<kAhead>(st, sh, maps, used, warp, first, kWarps, first < last ? (last - first + kWarps - 1) / kWarps : 0, []() { __syncthreads(); });
-  publish<T, D, NT>(sh, st, warp, lane);
+  walk.template run<kAhead, kWarps>(st, sh, maps, used, warp, first, kWarps, first < last ? (last - first + kWarps - 1) / kWarps : 0, []() { __syncthreads(); });
+  publish<T, D, NT, kWarps>(sh, st, warp, lane);
   __syncthreads();
   float* part = a.partials + (int64_t)cta * (8 * NT * (D + 2));
   const bool keep = !gave_up<T, NT>(p);
-  for (int i = tid; i < r.rows * a.Gi * D; i += kThreads) {
+  for (int i = 4 * tid; i < r.rows * a.Gi * D; i += 4 * kThreads) {
     const int col = i / D, c = i % D;
-    float n, w, acc;
-    combine_warps<T, D, NT>(sh, col, c, n, w, acc);
-    if (r.parts == 1) {
-      if (keep) write_out<T>(p, a, r.row0, r.item, col, c, n, w, acc);
-    } else {
-      part[i] = acc;
-      if (c == 0) {
-        part[8 * NT * D + col] = n;
-        part[8 * NT * (D + 1) + col] = w;
-      }
-    }
+    float n, w;
+    float4 acc;
+    combine_warps<T, D, NT, kWarps>(sh, col, c, n, w, acc);
+    if (r.parts > 1) store_part<D, NT>(part, col, c, n, w, acc);
+    else if (keep) write_out<T>(p, a, r.row0, r.item, col, c, n, w, acc);
   }
   end(p);
 }
@@ -841,40 +874,35 @@ __global__ void __launch_bounds__(kJoinThreads) paged_decode_join_shares_kernel(
   grid_go();
   grid_wait();
   const int4 j = __ldcg(a.joins + blockIdx.x);  // parts (0: none), first row, rows, item
-  const int i = blockIdx.y * kJoinThreads + threadIdx.x;
+  const int i = 4 * (blockIdx.y * kJoinThreads + threadIdx.x);
   if (i >= j.z * a.Gi * D || j.x == 0 || gave_up<T, NT>(p)) return;
-  const int col = i / D, c = i % D;
-  auto part = [&](int k) { return a.partials + (int64_t)(blockIdx.x + k * a.items) * (8 * NT * (D + 2)); };
-  float n = -INFINITY, w = 0.f, acc = 0.f;
-#pragma unroll 4
-  for (int k = 0; k < j.x; ++k) n = fmaxf(n, __ldcg(part(k) + 8 * NT * D + col));
-  const float n_use = n == -INFINITY ? 0.f : n;
-#pragma unroll 4
-  for (int k = 0; k < j.x; ++k) {
-    const float* q = part(k);
-    const float f = ex2f(__ldcg(q + 8 * NT * D + col) - n_use);
-    w = fmaf(f, __ldcg(q + 8 * NT * (D + 1) + col), w);
-    acc = fmaf(f, __ldcg(q + i), acc);
-  }
-  write_out<T>(p, a, j.y, j.w, col, c, n, w, acc);
+  float n, w;
+  float4 acc;
+  combine_parts<D, NT>(j.x, [&](int k) { return a.partials + (int64_t)(blockIdx.x + k * a.items) * (8 * NT * (D + 2)); }, i / D, i, n, w, acc);
+  write_out<T>(p, a, j.y, j.w, i / D, i % D, n, w, acc);
 }
 
 // ---- ranges of equal length
+// Two CTAs of four warps an SM (four with heads of 64), so that one streams while the other starts an item or leaves one.  us, one CTA of
+// eight warps -> these, 32 / 8 heads of 128, single tokens: 24 sequences of 250 to 2500 rows 46 -> 37, 64 of them 93 -> 80, 64 of 1000 to
+// 16384 376 -> 368; drafts of 2 to 6 rows, 64 of 250 to 2500 100 -> 94; 64 / 8 heads, 24 of 2 to 4 rows 60 -> 50.  (A thread had one output
+// at a time when the shares are added up, here and in the joining kernels; with four side by side the last was 94.)
 template <typename T, int D, int NT, int kAhead>
-__global__ void __launch_bounds__(kThreads, sizeof(T) == 2 && D == 64 && !kStaged<T, NT> ? 2 : 1) paged_decode_ranges_kernel(const __grid_constant__ AttnParams p, const __grid_constant__ DecodeArgs a,
+__global__ void __launch_bounds__(kRangeThreads, sizeof(T) == 2 && D == 64 && !kStaged<T, NT> ? 4 : 2) paged_decode_ranges_kernel(const __grid_constant__ AttnParams p, const __grid_constant__ DecodeArgs a,
     const __grid_constant__ MapsOf<T, NT> maps) {
   extern __shared__ __align__(16) uint8_t smem[];
-  SharedOf<T, D, NT>& sh = shared_of<T, D, NT>(smem);
-  __shared__ int s_group[kMaxGroups + 1];  // blocks (of one item) of the groups of 32 sequences before
+  SharedOf<T, D, NT, kRangeWarps>& sh = shared_of<T, D, NT, kRangeWarps>(smem);
+  int* s_group = reinterpret_cast<int*>(&sh);  // blocks (of one item) of the groups of 32 sequences before; rows and outputs come here later
+  static_assert((kMaxGroups + 1) * 4 <= kRangeWarps * 8 * NT * (D + 4) * 4, "");
   __shared__ RangeStart s_start;
   const PagedDev& g = p.paged;
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, cta = blockIdx.x;
-  set_up<T, D, NT>(sh, warp, lane);
+  set_up<T, D, NT, kRangeWarps>(sh, warp, lane);
   uint32_t used = 0;
   begin(p);
-  if (warp == kWarps - 1) clear_empty<T, D>(p, cta, a.n_cta, lane);
+  if (warp == kRangeWarps - 1) clear_empty<T, D>(p, cta, a.n_cta, lane);
   const int groups = (g.batch + 31) / 32;
-  for (int i = warp; i < groups; i += kWarps) {
+  for (int i = warp; i < groups; i += kRangeWarps) {
     const int b = i * 32 + lane, n = b < g.batch ? blocks_of(g, b) : 0;
     const int sum = __reduce_add_sync(0xffffffffu, n);
     if (lane == 0) s_group[i] = sum;
@@ -952,25 +980,19 @@ __global__ void __launch_bounds__(kThreads, sizeof(T) == 2 && D == 64 && !kStage
     State<D, NT> st;
     clear(st);
     const int first = s0 + warp;
-    walk.template run<kAhead>(st, sh, maps, used, warp, first, kWarps, first < s1 ? (s1 - first + kWarps - 1) / kWarps : 0, []() { __syncthreads(); });
-    publish<T, D, NT>(sh, st, warp, lane);
+    walk.template run<kAhead, kRangeWarps>(st, sh, maps, used, warp, first, kRangeWarps, first < s1 ? (s1 - first + kRangeWarps - 1) / kRangeWarps : 0, []() { __syncthreads(); });
+    publish<T, D, NT, kRangeWarps>(sh, st, warp, lane);
     __syncthreads();
     const bool whole = s0 == 0 && s1 == blocks;
     float* part = a.partials + (int64_t)(cta * 2 + (s0 > 0 ? 0 : 1)) * (8 * NT * (D + 2));
     const bool keep = !gave_up<T, NT>(p);
-    for (int i = tid; i < cols * D; i += kThreads) {
+    for (int i = 4 * tid; i < cols * D; i += 4 * kRangeThreads) {
       const int col = i / D, c = i % D;
-      float n, w, acc;
-      combine_warps<T, D, NT>(sh, col, c, n, w, acc);
-      if (whole) {
-        if (keep) write_out<T>(p, a, rows.x, item, col, c, n, w, acc);
-      } else {
-        part[i] = acc;
-        if (c == 0) {
-          part[8 * NT * D + col] = n;
-          part[8 * NT * (D + 1) + col] = w;
-        }
-      }
+      float n, w;
+      float4 acc;
+      combine_warps<T, D, NT, kRangeWarps>(sh, col, c, n, w, acc);
+      if (!whole) store_part<D, NT>(part, col, c, n, w, acc);
+      else if (keep) write_out<T>(p, a, rows.x, item, col, c, n, w, acc);
     }
     left -= s1 - s0;
     s0 = 0;
@@ -987,9 +1009,9 @@ __global__ void __launch_bounds__(kThreads, sizeof(T) == 2 && D == 64 && !kStage
   end(p);
 }
 
-// CTA i adds up the item that is cut for the first time where range i + 1 starts.
+// CTA (i, y) adds up a share of the columns of the item that is cut for the first time where range i + 1 starts.
 template <typename T, int D, int NT>
-__global__ void __launch_bounds__(kThreads) paged_decode_join_kernel(const __grid_constant__ AttnParams p, const __grid_constant__ DecodeArgs a) {
+__global__ void __launch_bounds__(kJoinThreads) paged_decode_join_kernel(const __grid_constant__ AttnParams p, const __grid_constant__ DecodeArgs a) {
   grid_go();
   grid_wait();
   const int at = blockIdx.x + 1;
@@ -1003,20 +1025,12 @@ __global__ void __launch_bounds__(kThreads) paged_decode_join_kernel(const __gri
   while (last + 1 < n_ranges && start(last + 1) < u1) ++last;
   const int2 rows = paged_rows(p.paged, r.b);
   const int cols = rows.y * a.Gi;
-  auto part = [&](int i) { return a.partials + (int64_t)(i * 2 + (i == at - 1 ? 1 : 0)) * (8 * NT * (D + 2)); };
-  for (int i = threadIdx.x; i < cols * D; i += kThreads) {
-    const int col = i / D, c = i % D;
-    float n = -INFINITY, w = 0.f, acc = 0.f;
-    for (int k = at - 1; k <= last; ++k) n = fmaxf(n, __ldcg(part(k) + 8 * NT * D + col));
-    const float n_use = n == -INFINITY ? 0.f : n;
-    for (int k = at - 1; k <= last; ++k) {
-      const float* q = part(k);
-      const float f = ex2f(__ldcg(q + 8 * NT * D + col) - n_use);
-      w = fmaf(f, __ldcg(q + 8 * NT * (D + 1) + col), w);
-      acc = fmaf(f, __ldcg(q + i), acc);
-    }
-    write_out<T>(p, a, rows.x, r.item, col, c, n, w, acc);
-  }
+  const int i = 4 * (blockIdx.y * kJoinThreads + threadIdx.x);
+  if (i >= cols * D) return;
+  float n, w;
+  float4 acc;
+  combine_parts<D, NT>(last - at + 2, [&](int k) { return a.partials + (int64_t)((at - 1 + k) * 2 + (k == 0 ? 1 : 0)) * (8 * NT * (D + 2)); }, i / D, i, n, w, acc);
+  write_out<T>(p, a, rows.x, r.item, i / D, i % D, n, w, acc);
 }
 
 template <typename F>
@@ -1035,7 +1049,7 @@ cudaError_t with_shape(cascade_dtype_t dtype, int d, int columns, F f) {
 }
 
 // CTAs that are resident at a time
-int ranges_cta(cascade_dtype_t dtype, int d, int columns) { return d == 128 || dtype == CASCADE_F32 || columns > kMostInRegisters ? 148 : 296; }
+int ranges_cta(cascade_dtype_t dtype, int d, int columns) { return d == 128 || dtype == CASCADE_F32 || columns > kMostInRegisters ? 296 : 592; }
 int columns_most(cascade_dtype_t dtype) { return dtype == CASCADE_BF16 ? kMostColumns : 16; }
 // Clusters only where all of them are resident at once with a CTA per SM (of 16, 10, 8, 4, 2 CTAs 7, 11, 15, 33, 74 are), and, with more
 // than one sequence, only over short caches: it is not known here how long they are, and one long sequence would be left to its clusters.
@@ -1104,7 +1118,7 @@ cudaError_t launch_paged_decode(const AttnParams& p, cascade_dtype_t dtype, int 
   return with_shape(dtype, p.d, columns, [&](auto t, auto d, auto nt) {
     using T = decltype(t);
     constexpr int D = decltype(d)::value, NT = decltype(nt)::value;
-    constexpr int smem = kSmemBytes<T, D, NT>;
+    constexpr int smem = kSmemBytes<T, D, NT, kWarps>;
     MapsOf<T, NT> maps;
     if constexpr (kStaged<T, NT>) {
       if (!encode_blocks(&maps.k, p.k, p.ks, p) || !encode_blocks(&maps.v, p.v, p.vs, p)) {
@@ -1133,18 +1147,19 @@ cudaError_t launch_paged_decode(const AttnParams& p, cascade_dtype_t dtype, int 
       if (e != cudaSuccess) return e;
       e = launch_dependent(kernel, dim3(a.n_cta), kThreads, smem, 1, true, stream, p, a, maps);
       if (e != cudaSuccess) return e;
-      return launch_dependent(paged_decode_join_shares_kernel<T, D, NT>, dim3(a.n_cta, (rows * a.Gi * D + kJoinThreads - 1) / kJoinThreads), kJoinThreads, 0, 1, true, stream, p, a);
+      return launch_dependent(paged_decode_join_shares_kernel<T, D, NT>, dim3(a.n_cta, (rows * a.Gi * D / 4 + kJoinThreads - 1) / kJoinThreads), kJoinThreads, 0, 1, true, stream, p, a);
     }
     constexpr int kAhead = sizeof(T) == 2 ? (D == 128 && NT == 1 ? 2 : 1) : (D == 64 && NT == 1 ? 2 : 1);
     a.n_cta = ranges_cta(dtype, p.d, columns);
     a.starts = static_cast<RangeStart*>(workspace);
     a.partials = reinterpret_cast<float*>(a.starts + a.n_cta);
+    constexpr int range_smem = kSmemBytes<T, D, NT, kRangeWarps>;
     auto kernel = paged_decode_ranges_kernel<T, D, NT, kAhead>;
-    cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
+    cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, range_smem);
     if (e != cudaSuccess) return e;
-    e = launch_dependent(kernel, dim3(a.n_cta), kThreads, smem, 1, true, stream, p, a, maps);
+    e = launch_dependent(kernel, dim3(a.n_cta), kRangeThreads, range_smem, 1, true, stream, p, a, maps);
     if (e != cudaSuccess) return e;
-    return launch_dependent(paged_decode_join_kernel<T, D, NT>, dim3(a.n_cta - 1), kThreads, 0, 1, true, stream, p, a);
+    return launch_dependent(paged_decode_join_kernel<T, D, NT>, dim3(a.n_cta - 1, (rows * a.Gi * D / 4 + kJoinThreads - 1) / kJoinThreads), kJoinThreads, 0, 1, true, stream, p, a);
   });
 }
 
