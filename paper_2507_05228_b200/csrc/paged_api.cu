@@ -283,8 +283,8 @@ struct PagedRoute {
   bool tiles;
 };
 PagedRoute paged_route(const AttnParams& p, cascade_dtype_t dtype, int32_t max_rows) {
-  const int few = paged_decode_rows(p, dtype);
-  if (std::min(max_rows, p.paged.n_rows) <= few || paged_decode_splits(p, dtype, std::min(max_rows, p.paged.n_rows))) return {std::min(max_rows, p.paged.n_rows), false};
+  const int few = paged_decode_rows(p, dtype), rows = std::min(max_rows, p.paged.n_rows);
+  if (rows <= few || paged_decode_splits(p, dtype, rows)) return {rows, false};
   // One sequence has max_rows rows, unless they are padded.  In fp32 the kernel on tiles takes all: what adds up the parts of its keys
   // writes every row.
   return {p.paged.batch == 1 || dtype == CASCADE_F32 ? 0 : few, true};

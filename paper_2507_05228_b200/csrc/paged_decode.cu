@@ -6,8 +6,8 @@
 //   Up to 8 columns the fragments come straight from global memory, as in decode.cu, which says why.
 //   More leave no registers for rows on their way.  Every warp then has a ring of 24 KiB in shared memory, filled by TMA a block at a
 //   time (two requests of 16 rows each), and reads fragments by ldmatrix.  It waits for its own copies only; no warp waits for another.
-//   us, 32 / 8 heads of 128, 16 sequences over 3000 to 9000 rows (bytes: 61): 2 rows each 83, 4 89, 6 98, 8 119; before, from registers 83
-//   and 109, and from 5 rows on in tiles of 256 that are nearly empty 131.  Over 3000 to 9000, 4 sequences of 6 rows 52 -> 32.
+//   us, 32 / 8 heads of 128, 16 sequences over 3000 to 9000 rows (bytes: 61): 2 rows each 74, 4 80, 6 83, 8 84; before, from registers 83
+//   and 109, and from 5 rows on in tiles of 256 that are nearly empty 131.  4 sequences of 6 rows 52 -> 30.
 // The weights go into the second product as two bf16 parts, the upper 16 bits and the rest, so that they keep 16 bits of mantissa: the
 // loads are the limit, and with one part the rounding of few rows of weights was most of the error (2500 rows, 32 heads: 2.4e-3 of
 // the output, 1.7e-3 with two, which is its own rounding).  From 17 columns on the products are the limit: one part, rounded to nearest,
@@ -18,9 +18,10 @@
 //
 // How the keys are shared out (rules and times at cluster_size).  Lengths differ between sequences, and only the device knows them.
 //   Few (sequence, KV head) items over short caches, or one sequence: a cluster of CTAs has one and adds up in distributed shared
-//   memory; one launch.  So have many over caches that cannot be long, in clusters of one that come in turns.
+//   memory; one launch.
 //   Few otherwise: every item gets a CTA, and the other CTAs of the chip go to the items by their length; what the CTAs of an item
 //   leave is added up by a second, small kernel.
+//   Many over caches that cannot be long: a CTA an item, no joining.
 //   Many: the 16-key blocks of all items, one after another, are cut into as many equal ranges as CTAs are resident; an item that a
 //   range covers whole is finished there, one that is cut leaves partials for the second kernel.
 // Who has what follows from the lengths, which every CTA adds up for itself.
@@ -109,6 +110,9 @@ struct Shared<T, D, NT, W, true> {
 };
 template <typename T, int D, int NT, int W>
 using SharedOf = Shared<T, D, NT, W, kStaged<T, NT>>;
+// CTAs of kRangeWarps that an SM takes
+template <typename T, int D, int NT>
+constexpr int kHalfCtas = sizeof(T) == 2 && D == 64 && !kStaged<T, NT> ? 4 : 2;
 template <typename T, int D, int NT, int W>
 constexpr int kSmemBytes = (int)sizeof(SharedOf<T, D, NT, W>) + (kStaged<T, NT> ? 1024 : 0);  // the ring starts at a multiple of 1024
 
@@ -357,8 +361,8 @@ struct Walk {
   }
   // The same walk over rows that TMA brings.  `used`: blocks that the warp's ring has had.
   template <int W, typename Ready>
-  __device__ __forceinline__ void run_staged(State<D, NT>& st, SharedOf<T, D, NT, W>& sh, const PageMaps& maps, uint32_t& used, int warp, int first, int stride,
-                                             int count, Ready ready, const int* early = nullptr) const {
+  __device__ __forceinline__ void run_staged(State<D, NT>& st, SharedOf<T, D, NT, W>& sh, const PageMaps& maps, uint32_t& used, int warp,
+                                             int first, int stride, int count, Ready ready, const int* early = nullptr) const {
     constexpr int S = kStages<D>;
     const tc::WaitCtx<false, W> wc{tc::smem_u32(sh.words), p.paged.status};
     int pages = lane >= count ? 0 : early ? paged_checked(p.paged, b, *early) : page_of(first + lane * stride), pages_next = 0;
@@ -373,9 +377,10 @@ struct Walk {
       const int slot = (first + t * stride) * 16 % p.paged.page_size;
       tc::mbar_expect_tx(bar, 2 * kPartBytes<D>);
       auto load = [&](uint32_t dst, const CUtensorMap* map) {
-        asm volatile("cp.async.bulk.tensor.5d.shared::cta.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %2, %4, %5}], [%6];" ::"r"(dst),
-                     "l"(map), "r"(0), "r"(slot), "r"(g), "r"(page), "r"(bar)
-                     : "memory");
+        asm volatile(
+            "cp.async.bulk.tensor.5d.shared::cta.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %2, %4, %5}], [%6];" ::"r"(dst),
+            "l"(map), "r"(0), "r"(slot), "r"(g), "r"(page), "r"(bar)
+            : "memory");
       };
       load(to, &maps.k);
       load(to + kPartBytes<D>, &maps.v);
@@ -587,7 +592,8 @@ __device__ __forceinline__ void store_part(float* part, int col, int c, float n,
 
 // Output columns c .. c + 3 of (row, head) of column `col`: n and w in log2 units
 template <typename T>
-__device__ __forceinline__ void write_out(const AttnParams& p, const DecodeArgs& a, int row0, int item, int col, int c, float n, float w, const float4& acc) {
+__device__ __forceinline__ void write_out(const AttnParams& p, const DecodeArgs& a, int row0, int item, int col, int c, float n, float w,
+                                          const float4& acc) {
   const int r = col / a.Gi, row = row0 + r, head = item * a.Gi + col - r * a.Gi;
   T* o = static_cast<T*>(p.o_out) + (int64_t)row * p.os.token + (int64_t)head * p.os.head + c;
   const float4 v = w > 0.f ? make_float4(acc.x / w, acc.y / w, acc.z / w, acc.w / w) : make_float4(0.f, 0.f, 0.f, 0.f);
@@ -681,8 +687,9 @@ __device__ __forceinline__ void end(const AttnParams& p) {
 
 // ---- an item per cluster
 template <typename T, int D, int NT, int kAhead>
-__global__ void __launch_bounds__(kThreads, 1) paged_decode_cluster_kernel(const __grid_constant__ AttnParams p, const __grid_constant__ DecodeArgs a,
-    const __grid_constant__ MapsOf<T, NT> maps) {
+__global__ void __launch_bounds__(kThreads, 1)
+    paged_decode_cluster_kernel(const __grid_constant__ AttnParams p, const __grid_constant__ DecodeArgs a,
+                               const __grid_constant__ MapsOf<T, NT> maps) {
   extern __shared__ __align__(16) uint8_t smem[];
   SharedOf<T, D, NT, kWarps>& sh = shared_of<T, D, NT, kWarps>(smem);
   __shared__ __align__(16) float s_o[8 * NT * D + 4 * kClusterMost];
@@ -730,8 +737,8 @@ __global__ void __launch_bounds__(kThreads, 1) paged_decode_cluster_kernel(const
     float4 acc;
     combine_warps<T, D, NT, kWarps>(sh, i / D, i % D, n, w, acc);
     const int to = i / per_cta;
-    asm volatile("st.shared::cluster.v4.f32 [%0], {%1, %2, %3, %4};" ::"r"(there(&s_o[rank * per_cta + i - to * per_cta], to)), "f"(acc.x), "f"(acc.y), "f"(acc.z),
-                 "f"(acc.w)
+    asm volatile("st.shared::cluster.v4.f32 [%0], {%1, %2, %3, %4};" ::"r"(there(&s_o[rank * per_cta + i - to * per_cta], to)), "f"(acc.x),
+                 "f"(acc.y), "f"(acc.z), "f"(acc.w)
                  : "memory");
     for (int c = i % D; c < min(i % D + 4, n_cta); ++c) {
       asm volatile("st.shared::cluster.f32 [%0], %1;" ::"r"(there(&s_n[rank][i / D], c)), "f"(n) : "memory");
@@ -757,6 +764,46 @@ __global__ void __launch_bounds__(kThreads, 1) paged_decode_cluster_kernel(const
   end(p);
 }
 
+// ---- an item per CTA
+template <typename T, int D, int NT, int kAhead>
+__global__ void __launch_bounds__(kRangeThreads, kHalfCtas<T, D, NT>)
+    paged_decode_items_kernel(const __grid_constant__ AttnParams p, const __grid_constant__ DecodeArgs a,
+                               const __grid_constant__ MapsOf<T, NT> maps) {
+  extern __shared__ __align__(16) uint8_t smem[];
+  SharedOf<T, D, NT, kRangeWarps>& sh = shared_of<T, D, NT, kRangeWarps>(smem);
+  const int item = blockIdx.x, b = blockIdx.y, tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+  set_up<T, D, NT, kRangeWarps>(sh, warp, lane);
+  uint32_t used = 0;
+  begin(p);
+  const int early = Walk<T, D, NT>::early_page(p.paged, b, warp + lane * kRangeWarps);
+  const int len = paged_len(p.paged, b);
+  const int2 rows = paged_rows(p.paged, b);
+  if (rows.y > p.paged.most && p.alone && tid == 0) paged_report(p.paged.status, kBadRows, b, rows.y);
+  if (rows.y >= p.paged.least && rows.y <= p.paged.most) {
+    Queries<T, D, NT> queries;
+    queries.load(p, a, rows.x, rows.y, item, warp, lane);
+    const Walk<T, D, NT> walk = make_walk<T, D, NT>(p, a, b, rows.x, rows.y, len, item, lane);
+    State<D, NT> st;
+    clear(st);
+    const int blocks = (len + 15) / 16;
+    const int count = warp < blocks ? (blocks - warp + kRangeWarps - 1) / kRangeWarps : 0;
+    walk.template run<kAhead, kRangeWarps>(st, sh, maps, used, warp, warp, kRangeWarps, count, [&]() {
+      queries.store(sh, warp, lane);
+      __syncthreads();
+    }, &early);
+    publish<T, D, NT, kRangeWarps>(sh, st, warp, lane);
+    __syncthreads();
+    const int outputs = gave_up<T, NT>(p) ? 0 : rows.y * a.Gi * D;
+    for (int i = 4 * tid; i < outputs; i += 4 * kRangeThreads) {
+      float n, w;
+      float4 acc;
+      combine_warps<T, D, NT, kRangeWarps>(sh, i / D, i % D, n, w, acc);
+      write_out<T>(p, a, rows.x, item, i / D, i % D, n, w, acc);
+    }
+  }
+  end(p);
+}
+
 // Zeros for the rows over an empty cache, by one warp of CTA `cta`
 template <typename T, int D>
 __device__ __forceinline__ void clear_empty(const AttnParams& p, int cta, int n_cta, int lane) {
@@ -774,7 +821,7 @@ __device__ __forceinline__ void clear_empty(const AttnParams& p, int cta, int n_
 
 // ---- a share of one item per CTA
 // Every item that has blocks gets a CTA, and what is left of them goes to the items by their length.
-constexpr int kSets = 3;  // of 32 sequences
+constexpr int kSets = 2;  // of 32 sequences: as many as there can be items (shares)
 struct Share {
   int b, item, row0, rows, len;  // b -1: none
   int part, parts;
@@ -830,8 +877,9 @@ __device__ __forceinline__ Share share_of(const AttnParams& p, const DecodeArgs&
 }
 
 template <typename T, int D, int NT, int kAhead>
-__global__ void __launch_bounds__(kThreads, 1) paged_decode_shares_kernel(const __grid_constant__ AttnParams p, const __grid_constant__ DecodeArgs a,
-    const __grid_constant__ MapsOf<T, NT> maps) {
+__global__ void __launch_bounds__(kThreads, 1)
+    paged_decode_shares_kernel(const __grid_constant__ AttnParams p, const __grid_constant__ DecodeArgs a,
+                               const __grid_constant__ MapsOf<T, NT> maps) {
   extern __shared__ __align__(16) uint8_t smem[];
   SharedOf<T, D, NT, kWarps>& sh = shared_of<T, D, NT, kWarps>(smem);
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, cta = blockIdx.x;
@@ -851,8 +899,10 @@ __global__ void __launch_bounds__(kThreads, 1) paged_decode_shares_kernel(const 
   const Walk<T, D, NT> walk = make_walk<T, D, NT>(p, a, r.b, r.row0, r.rows, r.len, r.item, lane);
   State<D, NT> st;
   clear(st);
-  const int blocks = (r.len + 15) / 16, last = (int)((int64_t)blocks * (r.part + 1) / r.parts), first = (int)((int64_t)blocks * r.part / r.parts) + warp;
-  walk.template run<kAhead, kWarps>(st, sh, maps, used, warp, first, kWarps, first < last ? (last - first + kWarps - 1) / kWarps : 0, []() { __syncthreads(); });
+  const int64_t blocks = (r.len + 15) / 16;
+  const int last = (int)(blocks * (r.part + 1) / r.parts), first = (int)(blocks * r.part / r.parts) + warp;
+  const int count = first < last ? (last - first + kWarps - 1) / kWarps : 0;
+  walk.template run<kAhead, kWarps>(st, sh, maps, used, warp, first, kWarps, count, []() { __syncthreads(); });
   publish<T, D, NT, kWarps>(sh, st, warp, lane);
   __syncthreads();
   float* part = a.partials + (int64_t)cta * (8 * NT * (D + 2));
@@ -870,7 +920,8 @@ __global__ void __launch_bounds__(kThreads, 1) paged_decode_shares_kernel(const 
 
 // CTA (i, y) adds up a share of the columns of the item of which CTA i had the first part.
 template <typename T, int D, int NT>
-__global__ void __launch_bounds__(kJoinThreads) paged_decode_join_shares_kernel(const __grid_constant__ AttnParams p, const __grid_constant__ DecodeArgs a) {
+__global__ void __launch_bounds__(kJoinThreads) paged_decode_join_shares_kernel(const __grid_constant__ AttnParams p,
+                                                                const __grid_constant__ DecodeArgs a) {
   grid_go();
   grid_wait();
   const int4 j = __ldcg(a.joins + blockIdx.x);  // parts (0: none), first row, rows, item
@@ -878,7 +929,8 @@ __global__ void __launch_bounds__(kJoinThreads) paged_decode_join_shares_kernel(
   if (i >= j.z * a.Gi * D || j.x == 0 || gave_up<T, NT>(p)) return;
   float n, w;
   float4 acc;
-  combine_parts<D, NT>(j.x, [&](int k) { return a.partials + (int64_t)(blockIdx.x + k * a.items) * (8 * NT * (D + 2)); }, i / D, i, n, w, acc);
+  auto part = [&](int k) { return a.partials + (int64_t)(blockIdx.x + k * a.items) * (8 * NT * (D + 2)); };
+  combine_parts<D, NT>(j.x, part, i / D, i, n, w, acc);
   write_out<T>(p, a, j.y, j.w, i / D, i % D, n, w, acc);
 }
 
@@ -888,8 +940,9 @@ __global__ void __launch_bounds__(kJoinThreads) paged_decode_join_shares_kernel(
 // 16384 376 -> 368; drafts of 2 to 6 rows, 64 of 250 to 2500 100 -> 94; 64 / 8 heads, 24 of 2 to 4 rows 60 -> 50.  (A thread had one output
 // at a time when the shares are added up, here and in the joining kernels; with four side by side the last was 94.)
 template <typename T, int D, int NT, int kAhead>
-__global__ void __launch_bounds__(kRangeThreads, sizeof(T) == 2 && D == 64 && !kStaged<T, NT> ? 4 : 2) paged_decode_ranges_kernel(const __grid_constant__ AttnParams p, const __grid_constant__ DecodeArgs a,
-    const __grid_constant__ MapsOf<T, NT> maps) {
+__global__ void __launch_bounds__(kRangeThreads, kHalfCtas<T, D, NT>)
+    paged_decode_ranges_kernel(const __grid_constant__ AttnParams p, const __grid_constant__ DecodeArgs a,
+                               const __grid_constant__ MapsOf<T, NT> maps) {
   extern __shared__ __align__(16) uint8_t smem[];
   SharedOf<T, D, NT, kRangeWarps>& sh = shared_of<T, D, NT, kRangeWarps>(smem);
   int* s_group = reinterpret_cast<int*>(&sh);  // blocks (of one item) of the groups of 32 sequences before; rows and outputs come here later
@@ -980,7 +1033,8 @@ __global__ void __launch_bounds__(kRangeThreads, sizeof(T) == 2 && D == 64 && !k
     State<D, NT> st;
     clear(st);
     const int first = s0 + warp;
-    walk.template run<kAhead, kRangeWarps>(st, sh, maps, used, warp, first, kRangeWarps, first < s1 ? (s1 - first + kRangeWarps - 1) / kRangeWarps : 0, []() { __syncthreads(); });
+    const int count = first < s1 ? (s1 - first + kRangeWarps - 1) / kRangeWarps : 0;
+    walk.template run<kAhead, kRangeWarps>(st, sh, maps, used, warp, first, kRangeWarps, count, []() { __syncthreads(); });
     publish<T, D, NT, kRangeWarps>(sh, st, warp, lane);
     __syncthreads();
     const bool whole = s0 == 0 && s1 == blocks;
@@ -1011,7 +1065,8 @@ __global__ void __launch_bounds__(kRangeThreads, sizeof(T) == 2 && D == 64 && !k
 
 // CTA (i, y) adds up a share of the columns of the item that is cut for the first time where range i + 1 starts.
 template <typename T, int D, int NT>
-__global__ void __launch_bounds__(kJoinThreads) paged_decode_join_kernel(const __grid_constant__ AttnParams p, const __grid_constant__ DecodeArgs a) {
+__global__ void __launch_bounds__(kJoinThreads) paged_decode_join_kernel(const __grid_constant__ AttnParams p,
+                                                                const __grid_constant__ DecodeArgs a) {
   grid_go();
   grid_wait();
   const int at = blockIdx.x + 1;
@@ -1029,7 +1084,8 @@ __global__ void __launch_bounds__(kJoinThreads) paged_decode_join_kernel(const _
   if (i >= cols * D) return;
   float n, w;
   float4 acc;
-  combine_parts<D, NT>(last - at + 2, [&](int k) { return a.partials + (int64_t)((at - 1 + k) * 2 + (k == 0 ? 1 : 0)) * (8 * NT * (D + 2)); }, i / D, i, n, w, acc);
+  auto part = [&](int k) { return a.partials + (int64_t)((at - 1 + k) * 2 + (k == 0 ? 1 : 0)) * (8 * NT * (D + 2)); };
+  combine_parts<D, NT>(last - at + 2, part, i / D, i, n, w, acc);
   write_out<T>(p, a, rows.x, r.item, i / D, i % D, n, w, acc);
 }
 
@@ -1053,22 +1109,29 @@ int ranges_cta(cascade_dtype_t dtype, int d, int columns) { return d == 128 || d
 int columns_most(cascade_dtype_t dtype) { return dtype == CASCADE_BF16 ? kMostColumns : 16; }
 // Clusters only where all of them are resident at once with a CTA per SM (of 16, 10, 8, 4, 2 CTAs 7, 11, 15, 33, 74 are), and, with more
 // than one sequence, only over short caches: it is not known here how long they are, and one long sequence would be left to its clusters.
-// us, caches new to L2, 32 / 8 heads of 128 (clusters | shares | ranges, 6 us of them the events'): 4 sequences of 2500 rows 20 | 24 | 33,
-// of 8000 35 | 39 | 48, 6 of 1000 to 8000 52 | 40 | 45, of 30000 163 | 132 | 140, 16 of 300 17 | 20 | 26, of 1000 to 8000 92 | 94 | 75.
-// And a CTA an item, in turns, where no sequence can be long: the ranges pay for every item that they cross, and for the second kernel.
-// us, the same heads (CTAs | ranges): 32 sequences of 100 to 300 rows 14 | 24, 64 of 500 to 1000 51 | 57, 24 of 250 to 2000 37 | 44 but of
-// 1500 to 2000 48 | 45; drafts of 2 to 6 rows, 32 of 100 to 300 27 | 41, 64 of 1500 to 2000 109 | 114, 24 of 500 to 4000 72 | 74; fp32,
-// 64 of 40 to 160 31 | 48, of 900 to 1000 116 | 110.
-int cluster_size(const AttnParams& p, cascade_dtype_t dtype, int64_t items, int columns) {  // 0: shares or ranges
+// us, caches new to L2, 32 / 8 heads of 128 (clusters | shares, 6 us of them the events'): 4 sequences of 2500 rows 20 | 24, of 8000
+// 35 | 39, 6 of 1000 to 8000 52 | 40, of 30000 163 | 132, 16 of 300 17 | 20.
+int cluster_size(const AttnParams& p, int64_t items) {  // 0: shares or ranges
   const int64_t blocks = ((int64_t)p.paged.max_pages * p.paged.page_size + 15) / 16;
   int n = 0;
   for (const auto& fit : {std::pair<int, int>{148, 1}, {74, 2}, {33, 4}, {15, 8}, {11, 10}, {7, 16}})
     if (items <= fit.first) n = fit.second;
-  if (n == 0) return blocks <= (columns > 8 ? 16 : 8) * kWarps / (dtype == CASCADE_F32 ? 2 : 1) ? 1 : 0;
+  if (n == 0) return 0;
   n = (int)std::min<int64_t>(n, (blocks + kWarps - 1) / kWarps);
   return p.paged.batch == 1 || blocks <= 10 * kWarps * n ? n : 0;
 }
-bool shares(int64_t items) { return items <= 74; }  // two CTAs an item
+// And a CTA of four warps an item, one after another, where no sequence can be long: what is resident then evens out over the chip, and
+// nothing has to be joined.  us, the same heads, single tokens (these | ranges): 24 sequences of 40 to 160 rows 6.4 | 13, 40 of 200 to 1000
+// 29 | 32, 100 of them 54 | 64, 40 of 900 to 1000 44 | 39, 40 of 400 to 2000 54 | 47; drafts of 2 to 4 rows, 64 of 40 to 160 14 | 27, of 200
+// to 1000 41 | 52; fp32, 100 of 100 to 500 63 | 74, of 900 to 1000 148 | 148, 40 of them 93 | 69.
+bool one_each(const AttnParams& p, cascade_dtype_t dtype, int64_t items) {
+  return items > 148 && p.paged.batch <= 65535 && (int64_t)p.paged.max_pages * p.paged.page_size <= (dtype == CASCADE_F32 ? 512 : 1024);
+}
+// Shares where items are few: whole CTAs are a coarse measure of many items' lengths, and ranges cut few items into many parts.  us, single
+// tokens, the same heads (shares | ranges): 4 sequences of 1000 to 8000 rows 23 | 30, of 4000 to 30000 69 | 71, 6: 31 | 34 and 94 | 84, 8:
+// 44 | 39 and 139 | 103; 16 / 4 heads of 64, 9 of 1000 to 8000 18 | 28, 16 30 | 28; drafts of 2 to 6 rows, 6: 32 | 41 and 86 | 92, 8: 44 | 46
+// and 130 | 113, 9: 51 | 50 and 158 | 132.
+bool shares(int64_t items, int columns) { return items <= (columns > 16 ? 64 : 40); }
 
 bool encode_blocks(CUtensorMap* map, const void* base, const Strides& st, const AttnParams& p) {
   EncodeTiledFn fn = encode_tiled_fn();
@@ -1103,8 +1166,8 @@ size_t paged_decode_ws_bytes(const AttnParams& p, cascade_dtype_t dtype, int row
   const int heads = paged_decode_heads(p, dtype, rows);
   const int64_t items = (int64_t)p.paged.batch * (p.H / heads);
   const int columns = (rows * heads + 7) / 8 * 8, n = ranges_cta(dtype, p.d, columns);
-  if (cluster_size(p, dtype, items, columns) > 0) return 0;
-  if (shares(items)) return (size_t)n * (columns * (p.d + 2) * 4 + sizeof(int4));
+  if (one_each(p, dtype, items) || cluster_size(p, items) > 0) return 0;
+  if (shares(items, columns)) return (size_t)n * (columns * (p.d + 2) * 4 + sizeof(int4));
   return (size_t)n * (2 * columns * (p.d + 2) * 4 + sizeof(RangeStart));
 }
 
@@ -1113,7 +1176,7 @@ cudaError_t launch_paged_decode(const AttnParams& p, cascade_dtype_t dtype, int 
   a.Gi = paged_decode_heads(p, dtype, rows);
   a.items = p.H / a.Gi;
   const int64_t items = (int64_t)p.paged.batch * a.items;
-  const int columns = rows * a.Gi, cluster = cluster_size(p, dtype, items, columns);
+  const int columns = rows * a.Gi, cluster = cluster_size(p, items);
   TimedLaunch timed(stream);
   return with_shape(dtype, p.d, columns, [&](auto t, auto d, auto nt) {
     using T = decltype(t);
@@ -1126,10 +1189,19 @@ cudaError_t launch_paged_decode(const AttnParams& p, cascade_dtype_t dtype, int 
         return cudaErrorInvalidValue;
       }
     }
-    // Blocks ahead: as many as an SM has registers for.  bf16, heads of 128: two and a CTA per SM (one ahead and two CTAs keep as
+    // Blocks ahead: as many as an SM has registers for.  bf16, heads of 128: two, and eight warps an SM (one ahead and twice the warps keep as
     // many loads in flight, but the walk spills: 64 sequences of up to 16384 rows 466 us, 385 this way).
+    constexpr int kAhead = sizeof(T) == 4 && D == 128 ? 1 : 2;
+    constexpr int kAheadHalf = sizeof(T) == 2 ? (D == 128 && NT == 1 ? 2 : 1) : (D == 64 && NT == 1 ? 2 : 1);
+    constexpr int smem_half = kSmemBytes<T, D, NT, kRangeWarps>;
+    const int join_y = (rows * a.Gi * D / 4 + kJoinThreads - 1) / kJoinThreads;
+    if (one_each(p, dtype, items)) {
+      auto kernel = paged_decode_items_kernel<T, D, NT, kAheadHalf>;
+      const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem_half);
+      if (e != cudaSuccess) return e;
+      return launch_dependent(kernel, dim3(a.items, p.paged.batch), kRangeThreads, smem_half, 1, true, stream, p, a, maps);
+    }
     if (cluster > 0) {
-      constexpr int kAhead = sizeof(T) == 4 && D == 128 ? 1 : 2;
       auto kernel = paged_decode_cluster_kernel<T, D, NT, kAhead>;
       cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
       if (e == cudaSuccess && cluster > 8) e = cudaFuncSetAttribute(kernel, cudaFuncAttributeNonPortableClusterSizeAllowed, 1);
@@ -1137,8 +1209,7 @@ cudaError_t launch_paged_decode(const AttnParams& p, cascade_dtype_t dtype, int 
       a.n_cta = cluster;
       return launch_dependent(kernel, dim3(cluster, a.items, p.paged.batch), kThreads, smem, cluster, true, stream, p, a, maps);
     }
-    if (shares(items)) {
-      constexpr int kAhead = sizeof(T) == 4 && D == 128 ? 1 : 2;
+    if (shares(items, columns)) {
       a.n_cta = 148;
       a.joins = static_cast<int4*>(workspace);
       a.partials = reinterpret_cast<float*>(a.joins + a.n_cta);
@@ -1147,19 +1218,18 @@ cudaError_t launch_paged_decode(const AttnParams& p, cascade_dtype_t dtype, int 
       if (e != cudaSuccess) return e;
       e = launch_dependent(kernel, dim3(a.n_cta), kThreads, smem, 1, true, stream, p, a, maps);
       if (e != cudaSuccess) return e;
-      return launch_dependent(paged_decode_join_shares_kernel<T, D, NT>, dim3(a.n_cta, (rows * a.Gi * D / 4 + kJoinThreads - 1) / kJoinThreads), kJoinThreads, 0, 1, true, stream, p, a);
+      return launch_dependent(paged_decode_join_shares_kernel<T, D, NT>, dim3(a.n_cta, join_y), kJoinThreads, 0, 1, true, stream,
+                              p, a);
     }
-    constexpr int kAhead = sizeof(T) == 2 ? (D == 128 && NT == 1 ? 2 : 1) : (D == 64 && NT == 1 ? 2 : 1);
     a.n_cta = ranges_cta(dtype, p.d, columns);
     a.starts = static_cast<RangeStart*>(workspace);
     a.partials = reinterpret_cast<float*>(a.starts + a.n_cta);
-    constexpr int range_smem = kSmemBytes<T, D, NT, kRangeWarps>;
-    auto kernel = paged_decode_ranges_kernel<T, D, NT, kAhead>;
-    cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, range_smem);
+    auto kernel = paged_decode_ranges_kernel<T, D, NT, kAheadHalf>;
+    cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem_half);
     if (e != cudaSuccess) return e;
-    e = launch_dependent(kernel, dim3(a.n_cta), kRangeThreads, range_smem, 1, true, stream, p, a, maps);
+    e = launch_dependent(kernel, dim3(a.n_cta), kRangeThreads, smem_half, 1, true, stream, p, a, maps);
     if (e != cudaSuccess) return e;
-    return launch_dependent(paged_decode_join_kernel<T, D, NT>, dim3(a.n_cta - 1, (rows * a.Gi * D / 4 + kJoinThreads - 1) / kJoinThreads), kJoinThreads, 0, 1, true, stream, p, a);
+    return launch_dependent(paged_decode_join_kernel<T, D, NT>, dim3(a.n_cta - 1, join_y), kJoinThreads, 0, 1, true, stream, p, a);
   });
 }
 
