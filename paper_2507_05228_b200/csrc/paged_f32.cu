@@ -424,11 +424,17 @@ cudaError_t launch_d(const AttnParams& p, cudaStream_t stream) {
 
 }  // namespace
 
-// A CTA per SM, each with at least 256 keys of what the table can hold (us, two CTAs per SM and 512 keys | now: 3 drafts of 2 to 6 rows over
-// 646 to 672, 32 / 8 heads of 128, 37 | 25; 100 rows over 2000, 16 / 8 heads of 64, 47 | 32; 28 over 4000, 12 heads of 128, 64 | 44).
+// Keys of a tile are shared by as many CTAs, at least 256 keys of what the table can hold each, as make the rounds of a CTA per SM and the keys
+// of a CTA, with 256 for its start and its end, come out shortest.  (us, as many CTAs as fit in one round | so: 299 rows over 3725, 16 / 8
+// heads of 128, 80 tiles: 358 | 243; 512 over 4000, 12 heads of 64, 96 tiles: 183 | 129.  The 256, us, two CTAs per SM and 512 keys | one and
+// 256: 3 drafts of 2 to 6 rows over 646 to 672, 32 / 8 heads of 128, 37 | 25; 28 over 4000, 12 heads of 128, 64 | 44.)
 int paged_f32_parts(const AttnParams& p) {
   const int64_t ctas = tiles_bound(p, wide(p) ? 64 : 16) * (p.H >> heads_log2(p.G)), keys = (int64_t)p.paged.max_pages * p.paged.page_size;
-  return (int)std::max<int64_t>(1, std::min<int64_t>({kSms / std::max<int64_t>(1, ctas), keys / 256, 64}));
+  auto time = [&](int64_t parts) { return (ctas * parts + kSms - 1) / kSms * (keys / parts + 256); };
+  int64_t best = 1;
+  for (int64_t parts = 2; parts <= std::min<int64_t>(keys / 256, 64); ++parts)
+    if (time(parts) < time(best)) best = parts;
+  return time(best) * 10 < time(1) * 9 ? (int)best : 1;  // (joining the parts has to pay)
 }
 size_t paged_f32_ws_bytes(const AttnParams& p) {
   const int64_t parts = paged_f32_parts(p);
