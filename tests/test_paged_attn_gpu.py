@@ -139,6 +139,48 @@ def test_drafts_of_every_width(d, H, Hkv, n):
                 attend(b, visible=rng.integers(-3, 600, b.n), max_rows=rows)
 
 
+@pytest.mark.parametrize("d", [128, 64])
+@pytest.mark.parametrize("H,Hkv", [(5, 1), (7, 1), (8, 1), (16, 1), (24, 2), (28, 4), (40, 2)])
+@pytest.mark.parametrize("n", [1, 2, 6])
+def test_drafts_whose_heads_are_split(d, H, Hkv, n):
+    """More (row, head) pairs than a KV head's columns, few sequences: its heads go to several parts of the chip."""
+    for rows in (3, 5, 8):
+        lens = [700, 0, 33, 2500, 7, 160][:n]
+        news = [rows, 0, rows - 1, 1, rows, 2][:n]
+        for width in ([0, 900] if n > 1 else [0]):
+            b = pu.Batch(news, lens, H, Hkv, d, 32, seed=rows, **({"width": width} if width else {}))
+            attend(b, max_rows=rows)
+            attend(b, causal=False, max_rows=rows)
+
+
+@pytest.mark.parametrize("n", [3, 12, 40])
+@pytest.mark.parametrize("width", [0, 300])
+def test_captured_drafts_side_by_side(n, width):
+    """Two graphs with a workspace each, replayed on two streams over lengths that have changed: a CTA an item, shares, ranges."""
+    full = [300 + 37 * i % 600 for i in range(n)]
+    b = pu.Batch([1 + i % 6 for i in range(n)], full, 16, 4, 128, 32, seed=n, **({"width": width} if width else {}))
+    runs = []
+    for _ in range(2):
+        out, stream, graph = torch.zeros_like(b.q), torch.cuda.Stream(), torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph, stream=stream):
+            for _ in range(3):
+                _, lse = cb.cascade_attn_paged(b.q, b.k_pages, b.v_pages, b.table, b.row_start, b.kv_len, b.scale, max_rows=6, out=out)
+        runs.append((graph, stream, out, lse))
+    k_rows, v_rows = b.k_rows, b.v_rows
+    for cut in (0, 250, 290):
+        lens = [x - cut for x in full]
+        b.kv_len.copy_(pu.ints(lens))
+        b.lens, b.k_rows, b.v_rows = lens, [k[:x] for k, x in zip(k_rows, lens)], [v[:x] for v, x in zip(v_rows, lens)]
+        torch.cuda.synchronize()
+        for graph, stream, _, _ in runs:
+            with torch.cuda.stream(stream):
+                graph.replay()
+        torch.cuda.synchronize()
+        for _, _, out, lse in runs:
+            b.check(out, lse)
+    assert cb.cascade_paged_status() == 0
+
+
 def test_long_cache_and_many_sequences():
     attend(pu.Batch([1, 4], [20001, 9000], 8, 2, 128, 64, seed=1), max_rows=4)
     attend(pu.Batch([1] * 300, [1 + 7 * i % 200 for i in range(300)], 4, 2, 64, 16, seed=2), max_rows=1)
