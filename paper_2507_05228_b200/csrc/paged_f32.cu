@@ -18,7 +18,8 @@
 // where sequences have them, 16 otherwise (16 in the example above: 40 us).  Where CTAs are few, key_parts of them share the keys and
 // leave partials, which paged_combine_kernel adds up.
 // What bounds it: half the time of the CTA with the longest keys is its products (12288 of 8 cycles, four at a time), a fifth the
-// chain of look-ups and first loads.
+// chain of look-ups and first loads.  Long chunks take 12.9 cycles a product where the units take 8.3 (512 rows over 4000, 32 / 8 heads of
+// 128, 713 us; 327 at 96 TFLOP/s, a third of the rate of tf32).
 #include <algorithm>
 
 #include "paged.cuh"
