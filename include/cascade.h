@@ -476,7 +476,7 @@ cascade_status_t cascade_decode_step_rope(cascade_plan_t* plan, int32_t batch, i
 
 /* Reads and clears what the paged calls on the current device have reported (SYNCHRONISES the device).  *out_code: 0, a code of
  * 121 on for a bad index (BAD_MAP; the message names it and where it stood), or that of a bounded wait that gave up (TIMEOUT).
- * After a wait has given up, later tensor-core calls on paged caches write nothing until this has been called. */
+ * After a wait has given up, later bf16 calls of cascade_attn_paged may write nothing until this has been called. */
 cascade_status_t cascade_paged_status(int32_t* out_code);
 
 /*

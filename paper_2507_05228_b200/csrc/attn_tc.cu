@@ -250,7 +250,7 @@ struct TmaArgs {
 // one after another): the shards are walked as in the fused mode, but a tile never mixes two shards, and at a shard
 // boundary the softmax threads write that shard's (u, m, l) out and start over.  The query tile, the TMEM allocation,
 // the barriers and the K/V pipelines are set up once per query tile instead of once per (query tile, KV shard).
-template <int D, bool kRope, bool kWalk, bool kBoxes, bool kPaged>
+template <int D, bool kRope, bool kWalk, bool kBoxes, bool kPaged, bool kTwofold = false>
 __global__ void __launch_bounds__(kThreads, 1) attn_tc_kernel(const __grid_constant__ AttnParams p, int lg,
                                                               int tile_major, int lg_split, int early, int after_gather,
                                                               const __grid_constant__ TmaArgs tma) {
@@ -455,6 +455,10 @@ __global__ void __launch_bounds__(kThreads, 1) attn_tc_kernel(const __grid_const
             least = __reduce_min_sync(0xffffffffu, least);
             if (lane == 1 + s) seen = least;
           }
+          if (kTwofold && n_sub == 1) {
+            const int least = __shfl_sync(0xffffffffu, seen, 1);
+            if (lane == 2) seen = least;
+          }
           if (lane == 0) seen = most;
         }
       }
@@ -532,6 +536,9 @@ __global__ void __launch_bounds__(kThreads, 1) attn_tc_kernel(const __grid_const
   const uint32_t tmem = *tmem_slot;
   const int n_act = stream_info[0];  // kWalk: shards of which the CTA sees something
   const int n_tiles = stream_info[1];
+  // kTwofold (pages, no sequence with more rows than a sub-tile): the second sub-tile takes every second tile of keys for the same rows,
+  // and the two are added up at the end; alone, each step waits for its products and they for it.
+  const bool twofold = kTwofold && n_sub == 1 && n_tiles > 1;
   // not kWalk: first key and number of keys of this CTA's part of the stream
   const int key0 = kWalk ? 0 : tab->slot0[0], n_keys = kWalk ? 0 : tab->need[0];
   // MMA tiles of four chunks; only the last one is narrower, or with kWalk the last one of every shard (see TileSeq)
@@ -595,10 +602,11 @@ __global__ void __launch_bounds__(kThreads, 1) attn_tc_kernel(const __grid_const
       asm volatile("fence.proxy.async.shared::cta;" ::: "memory");  // generic-proxy writes -> tensor-core reads
       mbar_arrive(bar(Q_FULL + s));
     }
-    if (s < n_sub) {
+    bool finishes = s < n_sub;
+    if (finishes || twofold) {
       const int m = tid & 127;  // MMA row = TMEM lane
-      const int sub_row0 = row0 + s * R;
-      const int sub_nrows = min(R, nrows - s * R);
+      const int sub_row0 = row0 + (twofold ? 0 : s * R);
+      const int sub_nrows = twofold ? nrows : min(R, nrows - s * R);
       const int slot_local = m >> lg;
       const bool row_ok = slot_local < sub_nrows;
       const int slot = sub_row0 + (row_ok ? slot_local : 0);
@@ -710,9 +718,11 @@ __global__ void __launch_bounds__(kThreads, 1) attn_tc_kernel(const __grid_const
         m_true = -INFINITY;
         l_run = 0.f;
       };
-      for (int i = 0; i < n_tiles; ++i) {
+      const int step = twofold ? 2 : 1, n_mine = twofold ? (n_tiles - s + 1) >> 1 : n_tiles;
+      for (int i = 0; i < n_mine; ++i) {
+        const int at = kTwofold ? i * step + (twofold ? s : 0) : i;  // tile of the CTA's keys
         // kWalk: a tile holds chunks of one shard only; the cursor stands at the tile's first chunk
-        const int nch = kWalk ? min(4, cur.nc - cur.c) : tile_chunks(i);
+        const int nch = kWalk ? min(4, cur.nc - cur.c) : tile_chunks(at);
         const bool opens = kWalk ? cur.c == 0 : i == 0;  // first tile of a shard (kWalk) or of the stream
         const int kk_tile = kWalk ? tab->kk[cur.j] : 0;
         // kWalk: mask bookkeeping for the tile's four chunks, done before the wait so that it costs nothing: a chunk of shard
@@ -766,8 +776,8 @@ __global__ void __launch_bounds__(kThreads, 1) attn_tc_kernel(const __grid_const
         tmem_wait_ld();
         // The mask is applied through a bit mask so that the compiler can move several bits at a time into predicates.
         if constexpr (!kWalk) {
-          if (kNMax * (i + 1) > unmasked) {  // warp-uniform
-            const int mine = min(*my_seen, n_keys) - kNMax * i;  // visible columns of the tile
+          if (kNMax * (at + 1) > unmasked) {  // warp-uniform
+            const int mine = min(*my_seen, n_keys) - kNMax * at;  // visible columns of the tile
 #pragma unroll
             for (int ch = 0; ch < 4; ++ch) {
               const int lc_ch = mine - kChunk * ch;
@@ -941,10 +951,50 @@ __global__ void __launch_bounds__(kThreads, 1) attn_tc_kernel(const __grid_const
           l_fix += top_error();
         }
       }
+      if constexpr (kTwofold) {
+        if (twofold) {
+          auto left = [&](int32_t* words) { return reinterpret_cast<volatile float*>(words + kM + m); };  // columns that hold nothing else
+          volatile float *const m_1 = left(tab->kk), *const l_1 = left(tab->need), *const fix_1 = left(tab->slot0), *const top_1 = left(tab->first[1]);
+          if (s == 1) {
+            *m_1 = m_run;
+            *l_1 = l_run;
+            *fix_1 = l_fix;
+            *top_1 = m_true;
+            asm volatile("bar.arrive 1, 256;" ::: "memory");
+          } else {
+            wait_bar(wc, bar(O_FULL), 0u, 3, n_tiles);
+            wait_bar(wc, bar(O_FULL + 1), 0u, 3, n_tiles);
+            tc_fence_after();
+            asm volatile("bar.sync 1, 256;" ::: "memory");
+            const float m_all = fmaxf(m_run, *m_1), m_use = m_all == -INFINITY ? 0.f : m_all;
+            const float f_0 = ex2(m_run - m_use), f_1 = ex2(*m_1 - m_use);
+            l_run = l_run * f_0 + *l_1 * f_1;
+            l_fix = l_fix * f_0 + *fix_1 * f_1;
+            m_true = fmaxf(m_true, *top_1);
+            m_run = m_all;
+#pragma unroll 1
+            for (int cc = 0; cc < kD / 32; ++cc) {
+              uint32_t o[32], o_1[32];
+              CASCADE_TMEM_LD32(o_addr + (uint32_t)(cc * 32), o, 0);
+              CASCADE_TMEM_LD32(o_addr + (uint32_t)(kD + cc * 32), o_1, 0);
+              tmem_wait_ld();
+#pragma unroll
+              for (int j = 0; j < 32; ++j) o[j] = __float_as_uint(fmaf(__uint_as_float(o_1[j]), f_1, __uint_as_float(o[j]) * f_0));
+              CASCADE_TMEM_ST32(o_addr + (uint32_t)(cc * 32), o, 0);
+            }
+            tmem_wait_st();
+          }
+        }
+      }
       auto may_write = [&]() {  // asked after the last product; see goes_on
         return (n_tiles > 0 ? wc.load(1) : *reinterpret_cast<volatile const int32_t*>(wc.status)) == 0;
       };
-      if (!kWalk && split > 1) {
+      if (!finishes) {
+        if (split > 1) {
+          cluster_barrier();
+          cluster_barrier();
+        }
+      } else if (!kWalk && split > 1) {
         // ---- epilogue of a query tile whose keys were shared by the cluster: CTA r finishes columns r * cols .. of all
         // rows.  Every CTA sends it those columns of its accumulator and its row statistics (relative to its own m).
         const int lcols = (kD == 64 ? 6 : 7) - (31 - __clz(split)), cols = 1 << lcols, me = part_of_keys;
@@ -1160,9 +1210,9 @@ __global__ void __launch_bounds__(kThreads, 1) attn_tc_kernel(const __grid_const
         auto s_col = [&](int s, int i) {  // logit buffer of sub-tile s, tile i
           return tmem + (uint32_t)((kRing ? (2 * i + s) % 3 : s) * 128);
         };
-        auto issue_qk = [&](int s, int i, int n) {  // S_s = Q_s K(i)^T, n keys wide
-          const uint32_t q_lo = q_lo0 + (uint32_t)(s * (kTileBytes >> 4));
-          const uint32_t k_lo = k_lo0 + (uint32_t)((i % kKStages) * (kTileBytes >> 4));
+        auto issue_qk = [&](int s, int i, int n, int k_tile, int q_tile) {  // S_s = Q K^T for step i of sub-tile s, n keys wide
+          const uint32_t q_lo = q_lo0 + (uint32_t)(q_tile * (kTileBytes >> 4));
+          const uint32_t k_lo = k_lo0 + (uint32_t)((k_tile % kKStages) * (kTileBytes >> 4));
           const uint32_t idesc_qk = make_idesc(kM, n, 0, 0);
           if (leader) {
 #pragma unroll
@@ -1174,9 +1224,9 @@ __global__ void __launch_bounds__(kThreads, 1) attn_tc_kernel(const __grid_const
             mma_commit(s_full(s, i));
           }
         };
-        // O_s (+)= P_s V(i) over n keys; a tile that opens a shard (kWalk) or the stream starts the accumulator afresh
-        auto issue_pv = [&](int s, int i, int n, bool opens) {
-          const uint32_t v_lo = v_lo0 + (uint32_t)((i % kVStages) * (kTileBytes >> 4));
+        // O_s (+)= P_s V over n keys; a tile that opens a shard (kWalk) or the stream starts the accumulator afresh
+        auto issue_pv = [&](int s, int i, int n, bool opens, int v_tile) {
+          const uint32_t v_lo = v_lo0 + (uint32_t)((v_tile % kVStages) * (kTileBytes >> 4));
           const int ksteps = n >> 4;
           if (leader) {
 #pragma unroll
@@ -1205,11 +1255,32 @@ __global__ void __launch_bounds__(kThreads, 1) attn_tc_kernel(const __grid_const
         for (int s = 0; s < n_sub; ++s) {
           fed = fed && wait_bar(wc, bar(Q_FULL + s), 0u, 6);
           tc_fence_after();
-          if (fed) issue_qk(s, 0, n_cur);
+          if (fed) issue_qk(s, 0, n_cur, 0, s);
         }
         if (fed && leader) mma_commit(bar(K_EMPTY));
         int n_run = fed ? n_tiles : 0;
-        if constexpr (kRing) {
+        if (twofold) {  // tile j is step j / 2 of sub-tile j mod 2; the logits of as many tiles as there are buffers run ahead
+          auto logits = [&](int j) {
+            fed = fed && wait_bar(wc, bar(K_FULL + j % kKStages), (uint32_t)((j / kKStages) & 1), 7, j);
+            tc_fence_after();
+            if (!fed) return;
+            issue_qk(j & 1, j >> 1, kChunk * tile_chunks(j), j, 0);
+            if (leader) mma_commit(bar(K_EMPTY + j % kKStages));
+          };
+          constexpr int kLead = kRing ? 3 : 2;
+          for (int j = 1; j < min(kLead, n_tiles); ++j) logits(j);
+          if (!fed || !goes_on()) n_run = 0;
+          for (int j = 0; j < n_run && fed; ++j) {
+            const int s = j & 1, i = j >> 1;
+            fed = wait_bar(wc, bar(V_FULL + j % kVStages), (uint32_t)((j / kVStages) & 1), 4, j) && wait_bar(wc, p_full(s, i), s_parity(i), 5, j);
+            if (!fed) break;
+            tc_fence_after();
+            issue_pv(s, i, kChunk * tile_chunks(j), i == 0, j);
+            if (j >= n_run - 2 && leader) mma_commit(bar(O_FULL + s));
+            if (leader) mma_commit(bar(V_EMPTY + j % kVStages));
+            if (j + kLead < n_run) logits(j + kLead);
+          }
+        } else if constexpr (kRing) {
           // Order: QK_0(0) QK_1(0) QK_0(1), then per tile i: PV_0(i) QK_1(i+1) PV_1(i) QK_0(i+2).  QK_1(i+1) takes the
           // buffer PV_0(i) has read, QK_0(i+2) the one of PV_1(i); MMAs execute in issue order, so neither needs a
           // barrier.  K(j) is released after QK_1(j), the later of its two readers.
@@ -1223,7 +1294,7 @@ __global__ void __launch_bounds__(kThreads, 1) attn_tc_kernel(const __grid_const
           if (n_tiles > 1) {
             n_next = kChunk * seq.next(opens_next);
             wait_k(1);
-            if (fed) issue_qk(0, 1, n_next);
+            if (fed) issue_qk(0, 1, n_next, 1, 0);
             if (fed && last_sub == 0 && leader) mma_commit(bar(K_EMPTY + 1 % kKStages));
           }
           if (!fed || !goes_on()) n_run = 0;
@@ -1234,17 +1305,17 @@ __global__ void __launch_bounds__(kThreads, 1) attn_tc_kernel(const __grid_const
               fed = wait_bar(wc, p_full(s, i), s_parity(i), 5, i);
               if (!fed) break;
               tc_fence_after();
-              issue_pv(s, i, n_cur, opens_cur);
+              issue_pv(s, i, n_cur, opens_cur, i);
               if (i == n_run - 1 && leader) mma_commit(bar(O_FULL + s));
               if (s == last_sub && leader) mma_commit(bar(V_EMPTY + i % kVStages));
               if (s == 0 && n_sub == 2 && i + 1 < n_run) {
-                issue_qk(1, i + 1, n_next);
+                issue_qk(1, i + 1, n_next, i + 1, 1);
                 if (leader) mma_commit(bar(K_EMPTY + (i + 1) % kKStages));
               }
               if (s == last_sub && i + 2 < n_run) {
                 wait_k(i + 2);
                 if (!fed) break;
-                issue_qk(0, i + 2, n_2);
+                issue_qk(0, i + 2, n_2, i + 2, 0);
                 if (last_sub == 0 && leader) mma_commit(bar(K_EMPTY + (i + 2) % kKStages));
               }
             }
@@ -1268,7 +1339,7 @@ __global__ void __launch_bounds__(kThreads, 1) attn_tc_kernel(const __grid_const
             fed = wait_bar(wc, p_full(s, i), s_parity(i), 5, i);
             if (!fed) break;
             tc_fence_after();
-            issue_pv(s, i, n_cur, opens_cur);
+            issue_pv(s, i, n_cur, opens_cur, i);
             if (!has_next && leader) mma_commit(bar(O_FULL + s));
             if (kWalk && has_next && opens_next && leader) mma_commit(bar(O_RDY + s));
             if (s == n_sub - 1 && leader) mma_commit(bar(V_EMPTY + i % kVStages));
@@ -1278,7 +1349,7 @@ __global__ void __launch_bounds__(kThreads, 1) attn_tc_kernel(const __grid_const
                 if (!fed) break;
                 tc_fence_after();
               }
-              issue_qk(s, i + 1, n_next);
+              issue_qk(s, i + 1, n_next, i + 1, s);
               if (s == n_sub - 1 && leader) mma_commit(bar(K_EMPTY + (i + 1) % kKStages));
             }
           }
@@ -1492,11 +1563,13 @@ struct TcLaunch {
   bool after_gather;
   bool boxes;  // partials at head_dim 128
   bool paged;
+  bool twofold;
 };
 
 cudaError_t launch_kernel(const AttnParams& p, bool walk, const TcLaunch& l, int64_t n_tiles, const tc::TmaArgs& tma,
                           cudaStream_t stream) {
-  auto kernel = l.paged   ? (p.d == 64 ? tc::attn_tc_kernel<64, false, false, false, true> : tc::attn_tc_kernel<128, false, false, false, true>)
+  auto kernel = l.twofold ? (p.d == 64 ? tc::attn_tc_kernel<64, false, false, false, true, true> : tc::attn_tc_kernel<128, false, false, false, true, true>)
+                : l.paged ? (p.d == 64 ? tc::attn_tc_kernel<64, false, false, false, true> : tc::attn_tc_kernel<128, false, false, false, true>)
                 : p.d == 64 ? (walk ? tc::attn_tc_kernel<64, false, true, true, false> : tc::attn_tc_kernel<64, false, false, false, false>)
                 : p.rope  ? tc::attn_tc_kernel<128, true, false, false, false>
                 : !walk   ? tc::attn_tc_kernel<128, false, false, false, false>
@@ -1640,7 +1713,11 @@ cudaError_t launch_paged_tc(const AttnParams& p, int max_rows, cudaStream_t stre
   const int64_t fit[4] = {148, 148, 132, 120};
   for (int i = 1; i < 4; ++i)
     if ((least * heads) << i <= fit[i] && key_tiles >= (p.d == 64 ? 2 : 3) << i) lg_split = i;
-  const TcLaunch l = {lg, bound * heads <= 8 * (int64_t)sm_count(), lg_split, 0, false, false, true};
+  // Sequences of at most a sub-tile of rows (us, one sub-tile at work | both: 16 sequences of 16 rows over 3000 to 9000, 32 / 8 heads of 128,
+  // 129 | 89, 4 of them 48 | 39; 35 rows over 7432, 16 / 8 heads, 27 | 24).  As a kernel of its own: where tiles are full the choice costs
+  // them a hundredth (16 sequences of 1 to 701 rows, heads of 64, 98.0 -> 99.3).
+  const bool twofold = std::min<int64_t>(max_rows, g.n_rows) << lg <= 128;
+  const TcLaunch l = {lg, bound * heads <= 8 * (int64_t)sm_count(), lg_split, 0, false, false, true, twofold};
   return launch_kernel(p, false, l, bound, tma, stream);
 }
 

@@ -181,6 +181,30 @@ def test_captured_drafts_side_by_side(n, width):
     assert cb.cascade_paged_status() == 0
 
 
+@pytest.mark.parametrize("d", [128, 64])
+@pytest.mark.parametrize("H,Hkv", [(2, 2), (4, 1), (8, 1), (12, 2)])
+@pytest.mark.parametrize("n", [1, 3])
+def test_chunks_that_fill_one_sub_tile(d, H, Hkv, n):
+    """At most 128 (row, head) pairs a KV head: tiles of keys from one to many, an odd number of them, shared by clusters or not."""
+    group = H // Hkv
+    group = 2 if group == 6 else group  # heads that are stacked: a power of two
+    for pairs in (40, 100, 128):
+        rows = pairs // group
+        for lens in ([rows + 1, 128, 129], [257, 0, 300], [1500, 640, 641], [2999, 33, 385]):
+            news = [rows, max(1, rows - 7), rows]
+            b = pu.Batch(news[:n], lens[:n], H, Hkv, d, 32, seed=pairs, scale_k=8.0 if pairs == 100 else 1.0)
+            attend(b, max_rows=rows)
+            attend(b, causal=False, max_rows=rows)
+            attend(b, visible=np.random.default_rng(pairs).integers(-2, 3200, b.n), max_rows=rows)
+
+
+@pytest.mark.parametrize("d", [128, 64])
+def test_more_rows_than_announced_in_a_sub_tile(d):
+    """max_rows chooses kernels and nothing else on tiles: a sequence with more rows than it says is right all the same."""
+    b = pu.Batch([200, 40, 64], [700, 300, 64], 4, 2, d, 32, seed=3)
+    attend(b, max_rows=64)
+
+
 def test_long_cache_and_many_sequences():
     attend(pu.Batch([1, 4], [20001, 9000], 8, 2, 128, 64, seed=1), max_rows=4)
     attend(pu.Batch([1] * 300, [1 + 7 * i % 200 for i in range(300)], 4, 2, 64, 16, seed=2), max_rows=1)
