@@ -1568,6 +1568,10 @@ struct TcLaunch {
 
 cudaError_t launch_kernel(const AttnParams& p, bool walk, const TcLaunch& l, int64_t n_tiles, const tc::TmaArgs& tma,
                           cudaStream_t stream) {
+  if (l.lg_split > 0 && !l.tile_major) {  // the CTAs of a cluster lie along x, which is the tiles' there
+    set_error("tensor-core attention: clusters with the tiles on the fastest axis");
+    return cudaErrorInvalidValue;
+  }
   auto kernel = l.twofold ? (p.d == 64 ? tc::attn_tc_kernel<64, false, false, false, true, true> : tc::attn_tc_kernel<128, false, false, false, true, true>)
                 : l.paged ? (p.d == 64 ? tc::attn_tc_kernel<64, false, false, false, true> : tc::attn_tc_kernel<128, false, false, false, true>)
                 : p.d == 64 ? (walk ? tc::attn_tc_kernel<64, false, true, true, false> : tc::attn_tc_kernel<64, false, false, false, false>)
@@ -1717,7 +1721,11 @@ cudaError_t launch_paged_tc(const AttnParams& p, int max_rows, cudaStream_t stre
   // 129 | 89, 4 of them 48 | 39; 35 rows over 7432, 16 / 8 heads, 27 | 24).  As a kernel of its own: where tiles are full the choice costs
   // them a hundredth (16 sequences of 1 to 701 rows, heads of 64, 98.0 -> 99.3).
   const bool twofold = std::min<int64_t>(max_rows, g.n_rows) << lg <= 128;
-  const TcLaunch l = {lg, bound * heads <= 8 * (int64_t)sm_count(), lg_split, 0, false, false, true, twofold};
+  // `bound` counts a tile of every sequence and `least` of the few that must have one, so there can be clusters where the first is large (200
+  // single tokens and one chunk).  The CTAs of a cluster share a tile, which has to be on the slowest axis for that; it has room: with
+  // clusters there are at most 74 tiles' rows in all, 256 each.
+  const bool tile_major = lg_split > 0 || bound * heads <= 8 * (int64_t)sm_count();
+  const TcLaunch l = {lg, tile_major, lg_split, 0, false, false, true, twofold};
   return launch_kernel(p, false, l, bound, tma, stream);
 }
 

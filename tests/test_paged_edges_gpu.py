@@ -1,0 +1,35 @@
+"""Calls on paged caches that lie between the ordinary ones, against 64 bits."""
+import math
+
+import numpy as np
+import pytest
+import torch
+
+import paged_util as pu
+from paper_2507_05228_b200 import binding as cb
+
+pytestmark = pytest.mark.gpu
+
+
+def attend(b, causal=True, visible=None, max_rows=None, **more):
+    out = torch.full((b.n, b.H, b.d), 5.0, dtype=b.dtype, device="cuda")
+    before = out.clone()
+    o, lse = cb.cascade_attn_paged(b.q, b.k_pages, b.v_pages, b.table, b.row_start, b.kv_len, b.scale, causal=causal,
+                                   visible=None if visible is None else pu.ints(visible), max_rows=max_rows, out=out, **more)
+    assert o is out and cb.cascade_paged_status() == 0
+    b.check(out, lse, causal, visible, before)
+    return out, lse
+
+
+@pytest.mark.parametrize("d", [128, 64])
+@pytest.mark.parametrize("H,Hkv,tokens", [(32, 8, 199), (32, 8, 200), (8, 2, 700), (8, 2, 701)])
+@pytest.mark.parametrize("chunk,max_rows", [(300, None), (300, 300), (30, 30)])
+def test_a_chunk_beside_many_single_tokens(d, H, Hkv, tokens, chunk, max_rows):
+    """Few tiles there must be and many there could be, behind tables wide enough that the keys of a tile are shared by a cluster: an
+    even and an odd number of tiles that could be; chunks of two sub-tiles and of one."""
+    rng = np.random.default_rng(tokens + chunk)
+    lens = [int(x) for x in rng.integers(0, 70, tokens)] + [900 + chunk]
+    news = [1] * tokens + [chunk]
+    place = tokens // 3
+    lens[place], lens[-1], news[place], news[-1] = lens[-1], lens[place], news[-1], news[place]
+    attend(pu.Batch(news, lens, H, Hkv, d, 32, seed=d + chunk, width=200), max_rows=max_rows)
