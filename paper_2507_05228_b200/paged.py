@@ -17,7 +17,9 @@ from . import binding as cb
 
 
 class PagedCache:
-    """Pages [n_pages, page_size, n_kv_heads, head_dim] for K and V of every layer, allocated here and nowhere else."""
+    """Pages [n_pages, page_size, n_kv_heads, head_dim] for K and V of every layer, allocated here and nowhere else.  `table`, `kv_len`,
+    `refs` and `report` stay the same tensors as long as the cache lives, so a step captured in a graph goes on from one replay to the
+    next."""
 
     def __init__(self, n_layers: int, n_pages: int, page_size: int, n_kv_heads: int, head_dim: int, max_seqs: int, max_len: int,
                  dtype=torch.bfloat16, device="cuda"):
@@ -25,23 +27,32 @@ class PagedCache:
         self.k = [torch.empty((n_pages, page_size, n_kv_heads, head_dim), dtype=dtype, device=device) for _ in range(n_layers)]
         self.v = [torch.empty_like(t) for t in self.k]
         width = -(-max_len // page_size)
-        self.table = torch.full((max_seqs, width), -1, dtype=torch.int32, device=device)
-        self.kv_len = torch.zeros(max_seqs, dtype=torch.int32, device=device)
+        # the table and the lengths in one piece, and a second one for a step to write to
+        self._state, self._next = (torch.zeros(max_seqs * (width + 1), dtype=torch.int32, device=device) for _ in range(2))
+        (self.table, self.kv_len), (self._next_table, self._next_len) = (
+            (t[:max_seqs * width].view(max_seqs, width), t[max_seqs * width:]) for t in (self._state, self._next))
+        self.table.fill_(-1)
         self.refs = torch.zeros(n_pages, dtype=torch.int32, device=device)
         self.report = torch.zeros(4, dtype=torch.int32, device=device)  # of the last step, see cascade_pages_fork
 
     def step(self, source: torch.Tensor, add: torch.Tensor) -> torch.Tensor:
         """Sequence i goes on as sequence source[i] (int32 on the GPU, -1: none) with room for add[i] more rows, counted in kv_len
-        from here on.  Returns the pairs of pages copied.  `report` says whether it could be done; if not, nothing has changed."""
-        self.table, self.kv_len, self.refs, copies, self.report = cb.cascade_pages_fork(self.table, self.kv_len, source, add,
-                                                                                       self.n_pages, self.page_size)
+        from here on.  Returns the pairs of pages copied.  `report` says whether it could be done; if not, nothing has changed, and
+        no rows may be appended."""
+        copies = torch.empty((self.kv_len.shape[0], 2), dtype=torch.int32, device=self.table.device)
+        cb.cascade_pages_fork(self.table, self.kv_len, source, add, self.n_pages, self.page_size,
+                              out=(self._next_table, self._next_len, self.refs, copies, self.report))
         cb.cascade_pages_copy(self.k + self.v, copies)
+        self._state.copy_(self._next)
         return copies
 
     def compact(self) -> torch.Tensor:
         """Moves the held pages to the front of the pools; returns (held pages, moves, bad entries, free pages) as int32 [4]."""
-        self.table, self.refs, moves, report = cb.cascade_pages_compact(self.table, self.kv_len, self.n_pages, self.page_size)
+        moves = torch.empty((self.n_pages // 2, 2), dtype=torch.int32, device=self.table.device)
+        report = torch.empty_like(self.report)
+        cb.cascade_pages_compact(self.table, self.kv_len, self.n_pages, self.page_size, out=(self._next_table, self.refs, moves, report))
         cb.cascade_pages_copy(self.k + self.v, moves)
+        self.table.copy_(self._next_table)
         return report
 
     def append(self, layer: int, k: torch.Tensor, v: torch.Tensor, row_start: torch.Tensor, q: Optional[torch.Tensor] = None,
