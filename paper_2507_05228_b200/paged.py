@@ -42,7 +42,7 @@ class PagedCache:
         copies = torch.empty((self.kv_len.shape[0], 2), dtype=torch.int32, device=self.table.device)
         cb.cascade_pages_fork(self.table, self.kv_len, source, add, self.n_pages, self.page_size,
                               out=(self._next_table, self._next_len, self.refs, copies, self.report))
-        cb.cascade_pages_copy(self.k + self.v, copies)
+        self._copy(copies)
         self._state.copy_(self._next)
         return copies
 
@@ -51,9 +51,14 @@ class PagedCache:
         moves = torch.empty((self.n_pages // 2, 2), dtype=torch.int32, device=self.table.device)
         report = torch.empty_like(self.report)
         cb.cascade_pages_compact(self.table, self.kv_len, self.n_pages, self.page_size, out=(self._next_table, self.refs, moves, report))
-        cb.cascade_pages_copy(self.k + self.v, moves)
+        self._copy(moves)
         self.table.copy_(self._next_table)
         return report
+
+    def _copy(self, pairs: torch.Tensor) -> None:
+        pools = self.k + self.v
+        for i in range(0, len(pools), 256):  # as many as a call takes
+            cb.cascade_pages_copy(pools[i:i + 256], pairs)
 
     def append(self, layer: int, k: torch.Tensor, v: torch.Tensor, row_start: torch.Tensor, q: Optional[torch.Tensor] = None,
                positions=None, rope_table=None, interleaved: bool = False, q_out=None):

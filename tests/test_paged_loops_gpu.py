@@ -1,4 +1,4 @@
-"""Loops on PagedCache as a server runs them: steps captured in a graph and replayed."""
+"""Loops on PagedCache as a server runs them: steps captured in a graph and replayed, models of many layers."""
 import math
 
 import numpy as np
@@ -81,3 +81,25 @@ def test_a_captured_step_goes_on_from_replay_to_replay(dtype, d, page):
             report = cache.compact()
             assert report[2].item() == 0 and cache.refs[:report[0].item()].all().item()
     assert cb.cascade_paged_status() == 0
+
+
+def test_a_model_of_more_layers_than_a_copy_takes_pools():
+    layers, page, Hkv, d = 130, 16, 1, 64
+    cache = PagedCache(layers, 6, page, Hkv, d, 2, 64)
+    cache.step(pu.ints([-1, -1]), pu.ints([20, 0]))
+    first, second = cache.table[0, :2].tolist()
+    for x in range(layers):
+        cache.k[x].fill_(0)
+        cache.v[x].fill_(0)
+        cache.k[x][second], cache.v[x][second] = 1 + x, 1000 + x
+    cache.step(pu.ints([0, 0]), pu.ints([0, 1]))
+    assert cache.report[:3].tolist() == [0, 0, 0] and cache.table[0, :2].tolist() == [first, second]
+    mine = cache.table[1, 1].item()
+    assert cache.table[1, 0].item() == first and mine != second
+    for x in range(layers):
+        assert torch.equal(cache.k[x][mine], cache.k[x][second]) and torch.equal(cache.v[x][mine], cache.v[x][second]), x
+    cache.step(pu.ints([-1, 1]), pu.ints([0, 0]))
+    report = cache.compact()
+    assert report[:3].tolist() == [2, 1, 0] and sorted(cache.table[1, :2].tolist()) == [0, 1]
+    for x in range(layers):
+        assert (cache.k[x][cache.table[1, 1].item()] == 1 + x).all()
