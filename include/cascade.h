@@ -524,7 +524,8 @@ cascade_status_t cascade_rope_rows(cascade_dtype_t dtype, int32_t n_rows, int32_
  *              q_out may be q
  *   positions  DEVICE int32 [n_rows] or NULL: y itself.  (A party that holds some of the tokens gives the original ones.)
  *   rope_table NULL: rows are taken as they are
- * A row whose place, page or position is bad is reported and not written.  Errors: INVALID_ARG, UNSUPPORTED, CUDA.
+ * A row whose place, page or position is bad is reported and not written, and so are all rows of a sequence whose kv_len is negative or
+ * more than its row of the table has room for.  Errors: INVALID_ARG, UNSUPPORTED, CUDA.
  */
 cascade_status_t cascade_paged_append(cascade_dtype_t dtype, int32_t batch, int32_t n_rows, int32_t n_heads,
                                       int32_t n_kv_heads, int32_t head_dim, const void* q, cascade_strides_t q_strides,

@@ -106,9 +106,10 @@ __global__ void __launch_bounds__(256) rope_rows_kernel(const __grid_constant__ 
     if (s < 0) return;
     const int2 rows = paged_rows(p.paged, s);
     if (row < rows.x || row >= rows.x + rows.y) return;  // behind the last sequence
-    const int y = paged_len(p.paged, s) - rows.y + row - rows.x;  // its row of the cache
-    if (y < 0) {
-      if (lane == 0) paged_report(p.paged.status, kBadLength, s, y);
+    const int len = fresh(p.paged.kv_len + s), y = len - rows.y + row - rows.x;  // its row of the cache
+    const bool bad = len < 0 || len > (int64_t)p.paged.max_pages * p.paged.page_size;
+    if (bad || y < 0) {  // (a length cut to what the table holds would put the row over an older one)
+      if (lane == 0) paged_report(p.paged.status, kBadLength, s, bad ? len : y);
       return;
     }
     const int index = y / p.paged.page_size, slot = y - index * p.paged.page_size;

@@ -33,3 +33,24 @@ def test_a_chunk_beside_many_single_tokens(d, H, Hkv, tokens, chunk, max_rows):
     place = tokens // 3
     lens[place], lens[-1], news[place], news[-1] = lens[-1], lens[place], news[-1], news[place]
     attend(pu.Batch(news, lens, H, Hkv, d, 32, seed=d + chunk, width=200), max_rows=max_rows)
+
+
+@pytest.mark.parametrize("n", [1, 4])
+@pytest.mark.parametrize("over", [1, 40])
+def test_append_past_the_end_of_the_table_writes_nothing(n, over):
+    """A sequence that has grown past its row of the table: its new rows have no place, and the last ones that do are another's."""
+    b = pu.Batch([n, 2], [32, 20], 4, 2, 64, 16)
+    k, v = (torch.randn((b.n, 2, 64), device="cuda").to(torch.bfloat16) for _ in range(2))
+    b.table = b.table[:, :2].contiguous()
+    b.kv_len[0] = 32 + over
+    before = b.k_pages.clone(), b.v_pages.clone()
+    q_out = torch.full_like(b.q, 9.0)
+    cb.cascade_paged_append(k, v, b.k_pages, b.v_pages, b.table, b.row_start, b.kv_len, q=b.q, q_out=q_out)
+    with pytest.raises(cb.CascadeError, match=f"code 122.*sequence 0, value {32 + over}"):
+        cb.cascade_paged_status()
+    for pages, was in zip((b.k_pages, b.v_pages), before):
+        for page in b.table[0].tolist():
+            assert torch.equal(torch.nan_to_num(pages[page], nan=77.0), torch.nan_to_num(was[page], nan=77.0))
+    page = b.table[1, 1].item()
+    assert torch.equal(b.k_pages[page, 2:4], k[n:n + 2]) and torch.equal(b.v_pages[page, 2:4], v[n:n + 2])
+    assert (q_out[:n] == 9).all() and torch.equal(q_out[n:n + 2], b.q[n:n + 2])
