@@ -986,6 +986,8 @@ __global__ void __launch_bounds__(kThreads, 1) attn_tc_kernel(const __grid_const
           }
         }
       }
+      // Whether anything was seen.  kPaged: a sum that is not a number (of a query that is none) counts, and shows in the row.
+      auto sees_any = [](float l) { return kPaged ? !(l == 0.f) : l > 0.f; };
       auto may_write = [&]() {  // asked after the last product; see goes_on
         return (n_tiles > 0 ? wc.load(1) : *reinterpret_cast<volatile const int32_t*>(wc.status)) == 0;
       };
@@ -1051,7 +1053,7 @@ __global__ void __launch_bounds__(kThreads, 1) attn_tc_kernel(const __grid_const
             if constexpr (kLateMax) fix_all += f_of[i] * *reinterpret_cast<const float*>(got_stats + i * 2 * kM * 16 + 8);
           }
         }
-        const float inv = l_all > 0.f ? 1.f / (l_all + fix_all) : 0.f;
+        const float inv = sees_any(l_all) ? 1.f / (l_all + fix_all) : 0.f;
         __nv_bfloat16* dst = static_cast<__nv_bfloat16*>(p.o_out) + b_rows * p.os.batch + (int64_t)(seq_row0 + slot) * p.os.token +
                              (int64_t)head * p.os.head + me * cols;
         for (int c0 = 0; c0 < cols; c0 += 8) {
@@ -1085,7 +1087,7 @@ __global__ void __launch_bounds__(kThreads, 1) attn_tc_kernel(const __grid_const
         }
         if (out_ok && me == 0 && p.lse_out)
           p.lse_out[(b_rows * pl.n_q + seq_row0 + slot) * p.H + head] =
-              l_all > 0.f ? (m_use + log2f(l_all)) * 0.6931471805599453f : -INFINITY;
+              sees_any(l_all) ? (m_use + log2f(l_all)) * 0.6931471805599453f : -INFINITY;
       } else {
       // ---- epilogue
       // Where this row goes is looked up before the wait for the last product, which hides the load.
@@ -1110,7 +1112,7 @@ __global__ void __launch_bounds__(kThreads, 1) attn_tc_kernel(const __grid_const
       if (n_tiles > 0) {
         wait_bar(wc, bar(O_FULL + s), 0u, 3, n_tiles);
         tc_fence_after();
-        if (l_run > 0.f) {
+        if (sees_any(l_run)) {
           o_scale = 1.f / (l_run + l_fix);
           l_out = l_run * ex2(m_run - m_true);  // sum relative to the exact max
           m_out = m_true * 0.6931471805599453f;   // natural-log units
@@ -1120,7 +1122,7 @@ __global__ void __launch_bounds__(kThreads, 1) attn_tc_kernel(const __grid_const
       if (quiet) dst = nullptr;
       if (dst) {
         if (p.fused) {
-          if (p.lse_out) p.lse_out[stat] = l_out > 0.f ? m_out + logf(l_out) : -INFINITY;
+          if (p.lse_out) p.lse_out[stat] = sees_any(l_out) ? m_out + logf(l_out) : -INFINITY;
         } else {
           p.m_part[stat] = m_out;
           p.l_part[stat] = l_out;

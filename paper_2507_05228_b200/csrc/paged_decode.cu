@@ -596,10 +596,11 @@ __device__ __forceinline__ void write_out(const AttnParams& p, const DecodeArgs&
                                           const float4& acc) {
   const int r = col / a.Gi, row = row0 + r, head = item * a.Gi + col - r * a.Gi;
   T* o = static_cast<T*>(p.o_out) + (int64_t)row * p.os.token + (int64_t)head * p.os.head + c;
-  const float4 v = w > 0.f ? make_float4(acc.x / w, acc.y / w, acc.z / w, acc.w / w) : make_float4(0.f, 0.f, 0.f, 0.f);
+  const bool none = w == 0.f;  // nothing is seen; a sum that is not a number shows in the row
+  const float4 v = none ? make_float4(0.f, 0.f, 0.f, 0.f) : make_float4(acc.x / w, acc.y / w, acc.z / w, acc.w / w);
   if constexpr (sizeof(T) == 2) *reinterpret_cast<uint2*>(o) = make_uint2(pack2_bf16(v.x, v.y), pack2_bf16(v.z, v.w));
   else *reinterpret_cast<float4*>(o) = v;
-  if (c == 0 && p.lse_out) p.lse_out[(int64_t)row * p.H + head] = w > 0.f ? n * 0.6931471805599453f + logf(w) : -INFINITY;
+  if (c == 0 && p.lse_out) p.lse_out[(int64_t)row * p.H + head] = none ? -INFINITY : n * 0.6931471805599453f + logf(w);
 }
 
 // The query fragments of item `item` of a sequence of `n` rows from row0 on, by warps 0 .. NT - 1.  Where latency is all (clusters) they

@@ -291,7 +291,8 @@ paged_f32_kernel(const __grid_constant__ AttnParams p, int lg, int tile_major) {
   // finished rows, or this part's share of them
   auto put = [&](int row, int col, float4 x, float m_raw, float w) {
     if (row >= n_rows) return;
-    const float inv = w > 0.f ? 1.f / w : 0.f;
+    const bool none = w == 0.f;  // nothing is seen; a sum that is not a number shows in the row
+    const float inv = none ? 0.f : 1.f / w;
     x.x *= inv;
     x.y *= inv;
     x.z *= inv;
@@ -301,12 +302,12 @@ paged_f32_kernel(const __grid_constant__ AttnParams p, int lg, int tile_major) {
       const int64_t stat = ((int64_t)key_part * p.paged.n_rows + tok) * p.H + head;
       *reinterpret_cast<float4*>(static_cast<float*>(p.o_part) + stat * D + col) = x;
       if (col == 0) {
-        p.m_part[stat] = w > 0.f ? m_raw * p.scale : -INFINITY;
+        p.m_part[stat] = none ? -INFINITY : m_raw * p.scale;
         p.l_part[stat] = w;
       }
     } else {
       *reinterpret_cast<float4*>(static_cast<float*>(p.o_out) + tok * p.os.token + head * p.os.head + col) = x;
-      if (col == 0 && p.lse_out) p.lse_out[tok * p.H + head] = w > 0.f ? m_raw * p.scale + logf(w) : -INFINITY;
+      if (col == 0 && p.lse_out) p.lse_out[tok * p.H + head] = none ? -INFINITY : m_raw * p.scale + logf(w);
     }
   };
 #pragma unroll
@@ -372,7 +373,7 @@ __global__ void __launch_bounds__(256) paged_combine_kernel(const __grid_constan
   for (int k = 0; k < p.key_parts; ++k) n = fmaxf(n, fresh(p.m_part + k * all + item));
   for (int k = 0; k < p.key_parts; ++k) {
     const float l = fresh(p.l_part + k * all + item);
-    const float f = l > 0.f ? l * expf(fresh(p.m_part + k * all + item) - n) : 0.f;
+    const float f = l == 0.f ? 0.f : l * expf(fresh(p.m_part + k * all + item) - n);
     const float4 u = fresh(reinterpret_cast<const float4*>(static_cast<const float*>(p.o_part) + (k * all + item) * D + col));
     w += f;
     o.x = fmaf(f, u.x, o.x);
@@ -380,11 +381,11 @@ __global__ void __launch_bounds__(256) paged_combine_kernel(const __grid_constan
     o.z = fmaf(f, u.z, o.z);
     o.w = fmaf(f, u.w, o.w);
   }
-  const float inv = w > 0.f ? 1.f / w : 0.f;
+  const float inv = w == 0.f ? 0.f : 1.f / w;
   const int head = (int)(item - row * p.H);
   *reinterpret_cast<float4*>(static_cast<float*>(p.o_out) + row * p.os.token + head * p.os.head + col) =
       make_float4(o.x * inv, o.y * inv, o.z * inv, o.w * inv);
-  if (col == 0 && p.lse_out) p.lse_out[item] = w > 0.f ? n + logf(w) : -INFINITY;
+  if (col == 0 && p.lse_out) p.lse_out[item] = w == 0.f ? -INFINITY : n + logf(w);
 }
 
 constexpr int64_t kSms = 148;

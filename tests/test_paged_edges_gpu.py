@@ -54,3 +54,38 @@ def test_append_past_the_end_of_the_table_writes_nothing(n, over):
     page = b.table[1, 1].item()
     assert torch.equal(b.k_pages[page, 2:4], k[n:n + 2]) and torch.equal(b.v_pages[page, 2:4], v[n:n + 2])
     assert (q_out[:n] == 9).all() and torch.equal(q_out[n:n + 2], b.q[n:n + 2])
+
+
+def poison(b, bits_of):
+    """Elements of queries of some rows and heads by their bits; returns where (rows, heads)."""
+    bad = torch.zeros(b.n, b.H, dtype=torch.bool)
+    bits = b.q.view(torch.int32 if b.dtype == torch.float32 else torch.int16)
+    for i, row in enumerate(sorted({0, b.n - 4, (b.n - 4) // 2, (b.n - 4) // 3})):
+        bits[row, 3 * i % b.H, 7 * i % b.d] = bits_of[i]
+        bad[row, 3 * i % b.H] = True
+    return bad
+
+
+def shows_in_its_row_alone(b, bad, max_rows):
+    o_ref, lse_ref, off_o, off_lse = b.reference()  # of the queries as they were
+    o, lse = cb.cascade_attn_paged(b.q, b.k_pages, b.v_pages, b.table, b.row_start, b.kv_len, b.scale, max_rows=max_rows)
+    assert cb.cascade_paged_status() == 0
+    o, lse = o.cpu(), lse.cpu()
+    assert torch.isnan(o[bad]).all() and torch.isnan(lse[bad]).all()
+    fine = ~bad
+    fine[sum(b.rows):] = False
+    assert ((o.double() - o_ref).abs() <= off_o)[fine].all() and ((lse.double() - lse_ref).abs() <= off_lse)[fine].all()
+
+
+ROUTES = [([1] * 4, None), ([1] * 12, 2000), ([1] * 40, 2000), ([1] * 100, None), ([4, 1, 3, 2], None), ([4] * 12, 2000), ([6] * 30, 2000),
+          ([30] * 3, None), ([30, 25], 200), ([70, 3, 200, 1], None), ([130], 200)]
+
+
+@pytest.mark.parametrize("dtype,d", [(torch.bfloat16, 128), (torch.bfloat16, 64), (torch.float32, 64), (torch.float32, 128)])
+@pytest.mark.parametrize("news,width", ROUTES)
+def test_a_query_that_is_not_a_number_shows_in_its_row_alone(dtype, d, news, width):
+    """It is not a row that sees nothing, whose zeros and lse of -inf a merge would leave out."""
+    rng = np.random.default_rng(len(news) + d)
+    b = pu.Batch(news, [int(x) for x in rng.integers(200, 500, len(news))], 8, 2, d, 32, dtype, seed=5, width=width)
+    bad = poison(b, [0x7fc00000] * 4 if dtype == torch.float32 else [0x7fff, -1, 0x7fc0, 0x7f81])
+    shows_in_its_row_alone(b, bad, max(news))
