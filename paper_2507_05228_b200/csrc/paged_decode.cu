@@ -637,10 +637,10 @@ struct Queries {
         sh.q[warp].step[2 * c + 1][lane] = make_uint2(x[c].z, x[c].w);
       } else {
         uint4 f0, f1;
-        cut_rounded(__uint_as_float(x[c].x), f0.x, f0.z);
-        cut_rounded(__uint_as_float(x[c].y), f0.y, f0.w);
-        cut_rounded(__uint_as_float(x[c].z), f1.x, f1.z);
-        cut_rounded(__uint_as_float(x[c].w), f1.y, f1.w);
+        cut_query(__uint_as_float(x[c].x), f0.x, f0.z);
+        cut_query(__uint_as_float(x[c].y), f0.y, f0.w);
+        cut_query(__uint_as_float(x[c].z), f1.x, f1.z);
+        cut_query(__uint_as_float(x[c].w), f1.y, f1.w);
         sh.q[warp].step[2 * c][lane] = f0;
         sh.q[warp].step[2 * c + 1][lane] = f1;
       }

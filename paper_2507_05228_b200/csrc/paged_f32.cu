@@ -144,10 +144,10 @@ paged_f32_kernel(const __grid_constant__ AttnParams p, int lg, int tile_major) {
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
       const float4 x = *reinterpret_cast<const float4*>(sQ + (wrow + 16 * mt + g + 8 * i) * C::kQPitch + 16 * c + 4 * t);
-      cut_rounded(x.x, hi[0][i], lo[0][i]);
-      cut_rounded(x.y, hi[0][2 + i], lo[0][2 + i]);
-      cut_rounded(x.z, hi[1][i], lo[1][i]);
-      cut_rounded(x.w, hi[1][2 + i], lo[1][2 + i]);
+      cut_query(x.x, hi[0][i], lo[0][i]);
+      cut_query(x.y, hi[0][2 + i], lo[0][2 + i]);
+      cut_query(x.z, hi[1][i], lo[1][i]);
+      cut_query(x.w, hi[1][2 + i], lo[1][2 + i]);
     }
   };
   float o[MT][D / 8][4];  // o[mt][4 j + q][2 i + h]: row wrow + 16 mt + g + 8 i, column 8 t + 4 h + q + 32 j

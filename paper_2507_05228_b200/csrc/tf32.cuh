@@ -18,9 +18,17 @@ __device__ __forceinline__ void cut(float x, uint32_t& hi, uint32_t& lo) {
   hi = __float_as_uint(x) & 0xffffe000u;
   lo = __float_as_uint(x - __uint_as_float(hi)) + 0x1000u;
 }
-__device__ __forceinline__ void cut_rounded(float x, uint32_t& hi, uint32_t& lo) {
+__device__ __forceinline__ void cut_rounded(float x, uint32_t& hi, uint32_t& lo) {  // x: at most 1
   hi = (__float_as_uint(x) + 0x1000u) & 0xffffe000u;
   lo = __float_as_uint(x - __uint_as_float(hi)) + 0x1000u;
+}
+// The same for any x.  Added to all ones, a NaN of the GPU's own, the half step would wrap around to zero, and the largest finite values
+// would become infinite: beyond what rounds to a finite value nothing is added.  NaN and infinities then have a lo that is NaN.
+// (512 fp32 rows over 4000, 32 / 8 heads of 128: 718 us without, so 729; by cvt.rna.satfinite 736.)
+__device__ __forceinline__ void cut_query(float x, uint32_t& hi, uint32_t& lo) {
+  const uint32_t half = fabsf(x) < 0x1.ffep127f ? 0x1000u : 0u;
+  hi = (__float_as_uint(x) + half) & 0xffffe000u;
+  lo = __float_as_uint(x - __uint_as_float(hi)) + half;
 }
 
 }  // namespace cascade

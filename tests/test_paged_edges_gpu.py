@@ -89,3 +89,32 @@ def test_a_query_that_is_not_a_number_shows_in_its_row_alone(dtype, d, news, wid
     b = pu.Batch(news, [int(x) for x in rng.integers(200, 500, len(news))], 8, 2, d, 32, dtype, seed=5, width=width)
     bad = poison(b, [0x7fc00000] * 4 if dtype == torch.float32 else [0x7fff, -1, 0x7fc0, 0x7f81])
     shows_in_its_row_alone(b, bad, max(news))
+
+
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("news,width", ROUTES)
+def test_every_not_a_number_of_an_fp32_query_counts(d, news, width):
+    """Those that arithmetic on the GPU makes among them, whose bits are all ones, and infinities."""
+    rng = np.random.default_rng(len(news) + d)
+    for bits in ([0x7fffffff, -1, 0x7fc00000, 0x7f800001], [0x7f800000, 0x7fffefff, 0x7ffff000, -0x800000]):
+        b = pu.Batch(news, [int(x) for x in rng.integers(200, 500, len(news))], 8, 2, d, 32, torch.float32, seed=5, width=width)
+        shows_in_its_row_alone(b, poison(b, bits), max(news))
+
+
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("news", [[1], [1] * 12, [5, 40], [100]])
+def test_the_largest_finite_queries_in_fp32(d, news):
+    """A query of the type's largest value times keys that bring the logit back to ordinary size."""
+    b = pu.Batch(news, [150 + i for i in range(len(news))], 4, 2, d, 32, torch.float32, seed=6)
+    largest = torch.finfo(torch.float32).max
+    b.q[:, 1] = 0
+    b.q[:, 1, 5] = largest
+    b.q64[:, 1] = 0
+    b.q64[:, 1, 5] = largest
+    table = b.table.cpu()
+    for s, x in enumerate(b.lens):
+        for y in range(x):
+            small = (1 + y % 8) * 2.0 ** -125
+            b.k_pages[table[s, y // 32].item(), y % 32, 0, 5] = small
+            b.k_rows[s][y, 0, 5] = small
+    attend(b)
