@@ -548,7 +548,7 @@ cascade_status_t cascade_paged_append(cascade_dtype_t dtype, int32_t batch, int3
  *              left as it was
  * A row that sees nothing yields zeros and lse = -inf.  (o_out, lse_out, 1) of one party is a partial (u, m, l) for cascade_merge
  * with those of others.  A query that holds a NaN yields NaN in its row and head of o_out and lse_out, and nowhere else.  Rows of the
- * cache that no length reaches may hold anything, NaN included.
+ * cache that no length reaches, and those that `visible` lets no row of their sequence see, may hold anything, NaN included.
  * bf16 and fp32, head_dim 64 and 128, n_heads a multiple of n_kv_heads.  K and V row starts must be 16-byte aligned, and for bf16
  * the strides of pages positive and below 2^38 elements.  scale positive and finite.  Rows of the cache that are seen hold finite
  * values.  fp32 operands are taken apart into two tf32 parts each, and products keep what lies above 2^-21 of themselves.

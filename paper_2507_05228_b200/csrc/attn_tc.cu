@@ -1395,10 +1395,14 @@ __global__ void __launch_bounds__(kThreads, 1) attn_tc_kernel(const __grid_const
         grid_wait();
         int n_issued = 0;
         // kPaged: where a box of this lane's comes from in tile i: row of the page and page; past the sequence's last row, where
-        // the table has no page, a page that does not exist, which reads as zeros
+        // the table has no page, a page that does not exist, which reads as zeros.  Rows that a given prefix leaves unseen may hold
+        // anything: the sequence ends before them.
+        int rows_end = seq_len;
+        if constexpr (kPaged)
+          if (p.paged.visible) rows_end = most_seen();
         auto box_of = [&](int i) {
           const int key = key0 + kNMax * i + (lane << tma.box_log2), index = key / p.paged.page_size;
-          const bool there = i < n_tiles && lane << tma.box_log2 < kNMax && key < seq_len;
+          const bool there = i < n_tiles && lane << tma.box_log2 < kNMax && key < rows_end;
           return make_int2(key - index * p.paged.page_size, there ? paged_page(p.paged, b, index) : p.paged.n_pages);
         };
         int2 box = make_int2(0, 0);
@@ -1416,7 +1420,7 @@ __global__ void __launch_bounds__(kThreads, 1) attn_tc_kernel(const __grid_const
           if constexpr (kPaged) {
             // The page in which the sequence ends holds anything behind its last row.  A key there is masked, but a weight of 0
             // times NaN is NaN: the values are overwritten with zeros before the tile counts as full.
-            const int end = seq_len - (key0 + kNMax * i), box_rows = 1 << tma.box_log2;
+            const int end = rows_end - (key0 + kNMax * i), box_rows = 1 << tma.box_log2;
             const bool tail = !is_k && end < kNMax && (end & (box_rows - 1)) != 0;
             const uint32_t arrives = tail ? bar(V_TAIL) : fb;
             if (leader) mbar_expect_tx(arrives, (uint32_t)kTileBytes);

@@ -450,6 +450,11 @@ struct Walk {
     __syncwarp();  // the ring may be written
   }
 
+  // how many of the blocks first, first + stride, .. lie below `last`, which is at most those of the sequence
+  __device__ __forceinline__ int count(int first, int stride, int last) const {
+    if (p.paged.visible) last = min(last, (len + 15) / 16);
+    return first < last ? (last - first + stride - 1) / stride : 0;
+  }
   // blocks first, first + stride, .. (count of them)
   template <int kAhead, int W, typename Ready>
   __device__ __forceinline__ void run(State<D, NT>& st, SharedOf<T, D, NT, W>& sh, const MapsOf<T, NT>& maps, uint32_t& used, int warp, int first,
@@ -648,6 +653,7 @@ struct Queries {
   }
 };
 
+// (With given prefixes the walk ends at the longest of its rows': what lies behind it may hold anything.  All lanes of a warp.)
 template <typename T, int D, int NT>
 __device__ __forceinline__ Walk<T, D, NT> make_walk(const AttnParams& p, const DecodeArgs& a, int b, int row0, int n, int len, int item, int lane) {
   const int x = lane >> 2, j = lane & 3, g = item * a.Gi / p.G;
@@ -660,6 +666,12 @@ __device__ __forceinline__ Walk<T, D, NT> make_walk(const AttnParams& p, const D
       const int r = (8 * nt + 2 * j + h) / a.Gi;
       w.lim[nt][h] = r < n ? paged_seen(p.paged, p.plan.causal, n, len, r, row0 + r) : 0;
     }
+  if (p.paged.visible) {
+    w.len = 0;
+#pragma unroll
+    for (int nt = 0; nt < NT; ++nt) w.len = max(w.len, max(w.lim[nt][0], w.lim[nt][1]));
+    w.len = __reduce_max_sync(0xffffffffu, w.len);
+  }
   return w;
 }
 template <int D, int NT>
@@ -719,7 +731,7 @@ __global__ void __launch_bounds__(kThreads, 1)
   const Walk<T, D, NT> walk = make_walk<T, D, NT>(p, a, b, rows.x, rows.y, len, item, lane);
   State<D, NT> st;
   clear(st);
-  walk.template run<kAhead, kWarps>(st, sh, maps, used, warp, first, stride, first < blocks ? (blocks - first + stride - 1) / stride : 0, [&]() {
+  walk.template run<kAhead, kWarps>(st, sh, maps, used, warp, first, stride, walk.count(first, stride, blocks), [&]() {
     queries.store(sh, warp, lane);
     __syncthreads();
   }, &early);
@@ -786,9 +798,7 @@ __global__ void __launch_bounds__(kRangeThreads, kHalfCtas<T, D, NT>)
     const Walk<T, D, NT> walk = make_walk<T, D, NT>(p, a, b, rows.x, rows.y, len, item, lane);
     State<D, NT> st;
     clear(st);
-    const int blocks = (len + 15) / 16;
-    const int count = warp < blocks ? (blocks - warp + kRangeWarps - 1) / kRangeWarps : 0;
-    walk.template run<kAhead, kRangeWarps>(st, sh, maps, used, warp, warp, kRangeWarps, count, [&]() {
+    walk.template run<kAhead, kRangeWarps>(st, sh, maps, used, warp, warp, kRangeWarps, walk.count(warp, kRangeWarps, (len + 15) / 16), [&]() {
       queries.store(sh, warp, lane);
       __syncthreads();
     }, &early);
@@ -902,8 +912,7 @@ __global__ void __launch_bounds__(kThreads, 1)
   clear(st);
   const int64_t blocks = (r.len + 15) / 16;
   const int last = (int)(blocks * (r.part + 1) / r.parts), first = (int)(blocks * r.part / r.parts) + warp;
-  const int count = first < last ? (last - first + kWarps - 1) / kWarps : 0;
-  walk.template run<kAhead, kWarps>(st, sh, maps, used, warp, first, kWarps, count, []() { __syncthreads(); });
+  walk.template run<kAhead, kWarps>(st, sh, maps, used, warp, first, kWarps, walk.count(first, kWarps, last), []() { __syncthreads(); });
   publish<T, D, NT, kWarps>(sh, st, warp, lane);
   __syncthreads();
   float* part = a.partials + (int64_t)cta * (8 * NT * (D + 2));
@@ -1034,8 +1043,7 @@ __global__ void __launch_bounds__(kRangeThreads, kHalfCtas<T, D, NT>)
     State<D, NT> st;
     clear(st);
     const int first = s0 + warp;
-    const int count = first < s1 ? (s1 - first + kRangeWarps - 1) / kRangeWarps : 0;
-    walk.template run<kAhead, kRangeWarps>(st, sh, maps, used, warp, first, kRangeWarps, count, []() { __syncthreads(); });
+    walk.template run<kAhead, kRangeWarps>(st, sh, maps, used, warp, first, kRangeWarps, walk.count(first, kRangeWarps, s1), []() { __syncthreads(); });
     publish<T, D, NT, kRangeWarps>(sh, st, warp, lane);
     __syncthreads();
     const bool whole = s0 == 0 && s1 == blocks;

@@ -118,3 +118,29 @@ def test_the_largest_finite_queries_in_fp32(d, news):
             b.k_pages[table[s, y // 32].item(), y % 32, 0, 5] = small
             b.k_rows[s][y, 0, 5] = small
     attend(b)
+
+
+def spoil_unseen(b, visible):
+    """NaN in the K and V rows of the caches that no row of their sequence sees, though the length reaches them."""
+    table = b.table.cpu()
+    for s in range(len(b.rows)):
+        seen = b.seen(s, True, visible)
+        for y in range(int(max(seen, default=0)), b.lens[s]):
+            b.k_pages[table[s, y // b.page].item(), y % b.page] = math.nan
+            b.v_pages[table[s, y // b.page].item(), y % b.page] = math.nan
+
+
+@pytest.mark.parametrize("dtype,d", [(torch.bfloat16, 128), (torch.bfloat16, 64), (torch.float32, 64), (torch.float32, 128)])
+@pytest.mark.parametrize("news,width", [([1] * 4, None), ([1] * 12, 2000), ([1] * 40, 2000), ([1] * 100, None), ([4, 1, 3, 2], None), ([8, 5, 1], None),
+                                        ([4] * 12, 2000), ([6] * 30, 2000), ([3] * 90, None), ([30] * 3, None), ([30, 25], 200), ([70, 3, 200, 1], None),
+                                        ([130], 200), ([33, 40], 200)])
+def test_rows_of_the_cache_that_a_prefix_leaves_unseen_may_hold_anything(dtype, d, news, width):
+    rng = np.random.default_rng(len(news) + d)
+    lens = [int(x) for x in rng.integers(30, 400 if len(news) < 40 else 200, len(news))]
+    b = pu.Batch(news, lens, 8, 2, d, 32, dtype, seed=4, width=width)
+    visible = np.full(b.n, 5)
+    for s in range(len(news)):
+        most = [0, lens[s] // 3, lens[s] - 1, lens[s]][rng.integers(0, 4)]
+        visible[b.starts[s]:b.starts[s + 1]] = rng.integers(0, most + 1, news[s])
+    spoil_unseen(b, visible)
+    attend(b, visible=visible, max_rows=max(news))
