@@ -471,7 +471,7 @@ cascade_status_t cascade_decode_step_rope(cascade_plan_t* plan, int32_t batch, i
  * not to be used.
  * New rows may only go to pages that one sequence holds (cascade_pages_fork sees to that).  Two calls that write the same pages, or
  * pages that the other reads, have to be ordered by the caller.  Make a first paged call on each device before one is captured (it
- * loads the kernels).  No sequence may have room for more than 2^30 rows.
+ * loads the kernels).  No sequence may have room for more than 2^30 rows, and in attention all of them together for 2^35 or more.
  */
 
 /* Reads and clears what the paged calls on the current device have reported (SYNCHRONISES the device).  *out_code: 0, a code of

@@ -67,6 +67,11 @@ cascade_status_t check_pages(const char* fn, int32_t batch, int32_t n_rows, int3
   if (!aligned4(table) || !aligned4(row_start) || !aligned4(kv_len)) return fail(CASCADE_ERR_INVALID_ARG, fn, "int32 arrays must be 4-byte aligned");
   return CASCADE_OK;
 }
+// Blocks of 16 rows of all sequences are counted in 32 bits (a page may stand in the table any number of times, so memory is no bound).
+cascade_status_t check_blocks(const char* fn, int32_t batch, int32_t page_size, int32_t max_pages) {
+  if ((int64_t)batch * ((int64_t)max_pages * page_size / 16) > INT_MAX) return fail(CASCADE_ERR_UNSUPPORTED, fn, "tables with room for 2^35 rows or more");
+  return CASCADE_OK;
+}
 PagedDev pages_dev(int32_t batch, int32_t n_rows, int32_t n_pages, int32_t page_size, const int32_t* table, int64_t table_stride,
                    int32_t max_pages, const int32_t* row_start, const int32_t* kv_len, const int32_t* visible) {
   PagedDev g;
@@ -309,6 +314,7 @@ cascade_status_t cascade_attn_paged_workspace_bytes(cascade_dtype_t dtype, int32
   if (batch < 1 || n_rows < 1 || max_rows < 1 || n_heads < 1 || n_kv_heads < 1 || max_pages < 1)
     return fail(CASCADE_ERR_INVALID_ARG, fn, "sizes must be positive");
   s = check_sizes(fn, n_heads, n_kv_heads, page_size, max_pages);
+  if (s == CASCADE_OK) s = check_blocks(fn, batch, page_size, max_pages);
   if (s != CASCADE_OK) return s;
   *out_bytes = paged_ws_bytes(paged_shape(batch, n_rows, max_rows, n_heads, n_kv_heads, head_dim, page_size, max_pages), dtype, max_rows);
   return CASCADE_OK;
@@ -329,6 +335,7 @@ cascade_status_t cascade_attn_paged(cascade_dtype_t dtype, int32_t batch, int32_
   if (s != CASCADE_OK) return s;
   if (max_rows < 1) return fail(CASCADE_ERR_INVALID_ARG, fn, "max_rows must be positive");
   s = check_sizes(fn, n_heads, n_kv_heads, page_size, max_pages);
+  if (s == CASCADE_OK) s = check_blocks(fn, batch, page_size, max_pages);
   if (s != CASCADE_OK) return s;
   if (!(scale > 0.f) || !std::isfinite(scale)) return fail(CASCADE_ERR_INVALID_ARG, fn, "scale must be positive and finite");
   const size_t es = elt_size(dtype);

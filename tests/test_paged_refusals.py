@@ -160,3 +160,13 @@ def test_the_binding_takes_tensors_of_the_current_device_only(L):
             call()
     with pytest.raises(TypeError):
         cb.cascade_rope_rows(None, pos, table)
+
+
+def test_more_rows_of_cache_than_32_bits_number_blocks_of(L):
+    """Sixteen rows are a block, and the blocks of all sequences are counted in 32 bits."""
+    S, G = cb.Strides(0, 512, 128), cb.Strides(16 * 512, 512, 128)
+    args = [1, 32, 32, 1, 8, 4, 128, 0.1, 1, P, S, P, G, P, G, 9, 16, P, 1 << 26, 1 << 26, P, P, None, P, S, None, P, 1 << 40, None]
+    refuses(L.cascade_attn_paged, args, 3, b"2^35")
+    n = ctypes.c_size_t()
+    assert L.cascade_attn_paged_workspace_bytes(1, 32, 32, 1, 8, 4, 128, 16, 1 << 26, ctypes.byref(n)) == 3
+    assert L.cascade_attn_paged_workspace_bytes(1, 31, 32, 1, 8, 4, 128, 16, 1 << 26, ctypes.byref(n)) == 0
