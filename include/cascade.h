@@ -544,8 +544,8 @@ cascade_status_t cascade_paged_append(cascade_dtype_t dtype, int32_t batch, int3
  *   causal     1: row i of the n of sequence b sees the cache rows y <= kv_len[b] - n + i;  0: all kv_len[b]
  *   visible    DEVICE int32 [n_rows] or NULL: the number of cache rows that a row sees instead (at most kv_len[b]); for a party
  *              whose pool holds the rows of a shard, VIS of its plan (cascade_shard_plan_resident)
- *   max_rows   no sequence has more rows; goes into the choice of kernels only, but a sequence with more is reported and may be
- *              left as it was
+ *   max_rows   no sequence has more rows; goes into the choice of kernels only.  A sequence with more is either reported and left as it
+ *              was (where the kernel for few rows is alone) or worked out like any other, and then not reported
  * A row that sees nothing yields zeros and lse = -inf.  (o_out, lse_out, 1) of one party is a partial (u, m, l) for cascade_merge
  * with those of others.  A query that holds a NaN yields NaN in its row and head of o_out and lse_out, and nowhere else.  Rows of the
  * cache that no length reaches, and those that `visible` lets no row of their sequence see, may hold anything, NaN included.

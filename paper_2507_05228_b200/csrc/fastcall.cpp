@@ -478,7 +478,9 @@ PyObject* attn_paged(PyObject* const* a) {
   const float scale = number(a[6]);
   const int32_t causal = truth(a[7]);
   const int32_t* visible = a[8] == Py_None ? nullptr : ints(here(a[8]), n, "visible is int32 [rows]");
-  const int32_t max_rows = a[9] == Py_None ? std::max(n, 1) : (int32_t)integer(a[9]);
+  const long long most = a[9] == Py_None ? std::max(n, 1) : integer(a[9]);
+  need(most >= INT32_MIN && most <= INT32_MAX, "max_rows is a 32-bit number");
+  const auto max_rows = (int32_t)most;
   const at::Tensor o = a[10] == Py_None ? at::empty_like(q) : here(a[10]);
   const cascade_strides_t os = row_strides(o);
   need(o.sizes() == q.sizes() && o.scalar_type() == q.scalar_type(), "out must be of q's shape and type");

@@ -144,3 +144,11 @@ def test_rows_of_the_cache_that_a_prefix_leaves_unseen_may_hold_anything(dtype, 
         visible[b.starts[s]:b.starts[s + 1]] = rng.integers(0, most + 1, news[s])
     spoil_unseen(b, visible)
     attend(b, visible=visible, max_rows=max(news))
+
+
+def test_max_rows_is_a_32_bit_number():
+    b = pu.Batch([2, 1], [30, 40], 4, 2, 64, 16)
+    for value in (2 ** 32 + 1, 2 ** 31, -2 ** 40):
+        with pytest.raises(ValueError, match="max_rows"):
+            cb.cascade_attn_paged(b.q, b.k_pages, b.v_pages, b.table, b.row_start, b.kv_len, b.scale, max_rows=value)
+    attend(b, max_rows=2 ** 31 - 1)
