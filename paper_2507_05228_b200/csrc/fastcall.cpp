@@ -111,6 +111,11 @@ at::Tensor lse_for(bool want, const at::Tensor& q) {
 }
 float* data_or_null(const at::Tensor& t) { return t.defined() ? static_cast<float*>(t.data_ptr()) : nullptr; }
 
+// Bytes of a workspace: no more than lie in its memory (a view may show the same ones many times).
+size_t bytes_of(const at::Tensor& t) {
+  const size_t es = t.element_size(), all = t.storage().nbytes(), before = (size_t)t.storage_offset() * es;
+  return std::min((size_t)t.numel() * es, all > before ? all - before : 0);
+}
 struct Scratch {
   at::Tensor own;
   void* ptr = nullptr;
@@ -124,7 +129,7 @@ Scratch scratch(const cascade_plan_t* plan, int call, cascade_dtype_t code, cons
   if (need == 0) return s;
   s.own = given == Py_None ? at::empty({(int64_t)need}, q.options().dtype(at::kByte)) : tensor(given);
   s.ptr = s.own.data_ptr();
-  s.bytes = (size_t)s.own.numel() * s.own.element_size();
+  s.bytes = bytes_of(s.own);
   return s;
 }
 
@@ -493,7 +498,7 @@ PyObject* attn_paged(PyObject* const* a) {
     if (bytes > 0) {
       ws.own = a[12] == Py_None ? at::empty({(int64_t)bytes}, q.options().dtype(at::kByte)) : here(a[12]);
       ws.ptr = ws.own.data_ptr();
-      ws.bytes = (size_t)ws.own.numel() * ws.own.element_size();
+      ws.bytes = bytes_of(ws.own);
     }
     void *st = stream(), *qp = q.data_ptr(), *op = o.data_ptr();
     float* lp = data_or_null(lse);

@@ -152,3 +152,13 @@ def test_max_rows_is_a_32_bit_number():
         with pytest.raises(ValueError, match="max_rows"):
             cb.cascade_attn_paged(b.q, b.k_pages, b.v_pages, b.table, b.row_start, b.kv_len, b.scale, max_rows=value)
     attend(b, max_rows=2 ** 31 - 1)
+
+
+def test_a_workspace_is_no_longer_than_its_memory():
+    """A view that shows the same bytes again and again."""
+    b = pu.Batch([1] * 40, [300] * 40, 8, 2, 64, 16, width=2000)
+    small = torch.zeros(256, dtype=torch.uint8, device="cuda")
+    for view in (small[:1].expand(1 << 26), small.expand(1 << 18, 256), small[:0]):
+        with pytest.raises(cb.CascadeError, match="workspace"):
+            cb.cascade_attn_paged(b.q, b.k_pages, b.v_pages, b.table, b.row_start, b.kv_len, b.scale, max_rows=1, workspace=view)
+    attend(b, max_rows=1, workspace=torch.zeros((1 << 13, 2 << 13), dtype=torch.uint8, device="cuda")[:, ::2])
