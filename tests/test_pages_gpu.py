@@ -201,3 +201,27 @@ def test_a_captured_step_follows_its_tables():
                 if a >= 0:
                     want_pool[b] = want_pool[a]
         assert torch.equal(pool, want_pool)
+
+
+@pytest.mark.parametrize("n_pages", [8200, 40000])
+@pytest.mark.parametrize("reader", [None, 5])
+def test_fork_of_one_prompt_by_as_many_sequences_as_there_may_be(n_pages, reader):
+    """8192 sequences that go on writing the second page of one prompt: the first keeps it, unless one only reads."""
+    n, page = 8192, 16
+    table, kv_len = np.full((n, 3), -1, np.int32), np.zeros(n, np.int32)
+    table[0, :2], kv_len[0] = (7, 2), 20
+    add = np.ones(n, np.int32)
+    if reader is not None:
+        add[reader] = 0
+    got = [t.cpu().numpy() for t in cb.cascade_pages_fork(pu.ints(table), pu.ints(kv_len), pu.ints(np.zeros(n)), pu.ints(add), n_pages, page)]
+    copies = add == 1
+    copies[0] = reader is not None
+    free = np.setdiff1d(np.arange(n_pages), [7, 2])
+    want, refs = np.tile([7, 2, -1], (n, 1)), np.zeros(n_pages, int)
+    want[copies, 1] = free[:copies.sum()]
+    refs[7], refs[2] = n, n - copies.sum()
+    refs[want[copies, 1]] = 1
+    pairs = np.full((n, 2), -1)
+    pairs[copies] = np.stack([np.full(copies.sum(), 2), want[copies, 1]], 1)
+    for g, w in zip(got, (want, 20 + add, refs, pairs, [0, 0, 0, free.size - copies.sum()])):
+        assert np.array_equal(g, w)
