@@ -581,7 +581,8 @@ cascade_status_t cascade_attn_paged_workspace_bytes(cascade_dtype_t dtype, int32
  *   report    DEVICE int32 [4], written: pages lacking; sequences that the table is too narrow for; bad entries (a source, a
  *             length, a page id, a negative add); pages left free.  Unless the first three are 0 nothing is done: the new state is
  *             the old one
- * One launch, no atomics whose order matters.  n_seqs at most 8192.  Errors: INVALID_ARG, UNSUPPORTED, CUDA.
+ * One launch, no atomics whose order matters.  n_seqs at most 8192, n_pages at most 2^30, n_seqs * width below 2^31.
+ * Errors: INVALID_ARG, UNSUPPORTED, CUDA.
  */
 cascade_status_t cascade_pages_fork(int32_t n_seqs, int32_t width, int32_t n_pages, int32_t page_size,
                                     const int32_t* table_in, const int32_t* kv_len_in, const int32_t* source,
@@ -595,7 +596,7 @@ cascade_status_t cascade_pages_fork(int32_t n_seqs, int32_t width, int32_t n_pag
  *   refs       as cascade_pages_fork, by the new ids
  *   moves      DEVICE int32 [n_pages / 2][2], written: (from, to) for cascade_pages_copy, then (-1, -1)
  *   report     DEVICE int32 [4], written: n_live; moves; bad entries (then nothing is moved); free pages
- * Errors: INVALID_ARG, CUDA.
+ * n_pages at most 2^30, n_seqs * width below 2^31.  Errors: INVALID_ARG, UNSUPPORTED, CUDA.
  */
 cascade_status_t cascade_pages_compact(int32_t n_seqs, int32_t width, int32_t n_pages, int32_t page_size,
                                        const int32_t* table_in, const int32_t* kv_len, int32_t* table_out, int32_t* refs,
@@ -608,8 +609,8 @@ cascade_status_t cascade_pages_compact(int32_t n_seqs, int32_t width, int32_t n_
  *   pools        HOST array of n_pools (at most 256) DEVICE pointers, 16-byte aligned
  *   page_strides HOST int64 [n_pools]: bytes from page to page, at least page_bytes
  *   page_bytes   bytes of a page, which is contiguous; a multiple of 16
- *   pairs        DEVICE int32 [n_pairs][2]
- * Errors: INVALID_ARG, UNSUPPORTED (more pools), CUDA.
+ *   pairs        DEVICE int32 [n_pairs][2], at most 2^30 of them
+ * Errors: INVALID_ARG, UNSUPPORTED (more pools or pairs), CUDA.
  */
 cascade_status_t cascade_pages_copy(int32_t n_pools, void* const* pools, const int64_t* page_strides, int64_t page_bytes,
                                     int32_t n_pages, const int32_t* pairs, int32_t n_pairs, void* stream);

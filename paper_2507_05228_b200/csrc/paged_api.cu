@@ -386,6 +386,9 @@ static cascade_status_t check_tables(const char* fn, int32_t n_seqs, int32_t wid
   if (!a || !b || !c || !d || !e || !f) return fail(CASCADE_ERR_INVALID_ARG, fn, "null pointer");
   if (n_seqs < 1 || width < 1 || n_pages < 1 || page_size < 1) return fail(CASCADE_ERR_INVALID_ARG, fn, "sizes must be positive");
   if ((int64_t)width * page_size > 1 << 30) return fail(CASCADE_ERR_UNSUPPORTED, fn, "a sequence of more than 2^30 rows");
+  // pages are walked, and what the sequences ask for is added up, in 32 bits
+  if (n_pages > 1 << 30) return fail(CASCADE_ERR_UNSUPPORTED, fn, "more than 2^30 pages");
+  if ((int64_t)n_seqs * width > INT_MAX) return fail(CASCADE_ERR_UNSUPPORTED, fn, "a table of 2^31 entries or more");
   if (a == b) return fail(CASCADE_ERR_INVALID_ARG, fn, "the new table may not be the old one");
   return CASCADE_OK;
 }
@@ -448,6 +451,7 @@ cascade_status_t cascade_pages_copy(int32_t n_pools, void* const* pools, const i
   if (!pools || !page_strides || (n_pairs > 0 && !pairs)) return fail(CASCADE_ERR_INVALID_ARG, fn, "null pointer");
   if (n_pools < 1 || n_pages < 1 || n_pairs < 0 || page_bytes < 16 || page_bytes % 16 != 0 || page_bytes > (int64_t)1 << 40)
     return fail(CASCADE_ERR_INVALID_ARG, fn, "sizes must be positive and page_bytes a multiple of 16");
+  if (n_pairs > 1 << 30) return fail(CASCADE_ERR_UNSUPPORTED, fn, "more than 2^30 pairs");
   if (n_pools > kMaxPools) {
     set_error("%s: %d pools, at most %d", fn, n_pools, kMaxPools);
     return CASCADE_ERR_UNSUPPORTED;

@@ -170,3 +170,13 @@ def test_more_rows_of_cache_than_32_bits_number_blocks_of(L):
     n = ctypes.c_size_t()
     assert L.cascade_attn_paged_workspace_bytes(1, 32, 32, 1, 8, 4, 128, 16, 1 << 26, ctypes.byref(n)) == 3
     assert L.cascade_attn_paged_workspace_bytes(1, 31, 32, 1, 8, 4, 128, 16, 1 << 26, ctypes.byref(n)) == 0
+
+
+def test_tables_beyond_32_bits(L):
+    fork = [4, 3, 9, 16, P, P, P, P, 2 * P, 2 * P, 3 * P, 4 * P, 5 * P, None]
+    compact = [4, 3, 9, 16, P, P, 2 * P, 3 * P, 4 * P, 5 * P, None]
+    for f, args in ((L.cascade_pages_fork, fork), (L.cascade_pages_compact, compact)):
+        refuses(f, args, 3, b"pages", _2=(1 << 30) + 1)
+        refuses(f, args, 3, b"entries", _0=8192, _1=1 << 18)
+    pools, strides = (ctypes.c_void_p * 1)(P), (ctypes.c_int64 * 1)(512)
+    refuses(L.cascade_pages_copy, [1, pools, strides, 512, 9, P, (1 << 30) + 1, None], 3, b"pairs")
