@@ -551,7 +551,10 @@ cascade_status_t cascade_paged_append(cascade_dtype_t dtype, int32_t batch, int3
  * cache that no length reaches, and those that `visible` lets no row of their sequence see, may hold anything, NaN included.
  * bf16 and fp32, head_dim 64 and 128, n_heads a multiple of n_kv_heads.  K and V row starts must be 16-byte aligned, and for bf16
  * the strides of pages positive and below 2^38 elements.  scale positive and finite.  Rows of the cache that are seen hold finite
- * values.  fp32 operands are taken apart into two tf32 parts each, and products keep what lies above 2^-21 of themselves.
+ * values.  bf16: the weights keep 16 bits of mantissa in the product with V for single tokens and for drafts whose max_rows times the
+ * heads of a KV head is at most 16, and with heads of 64 in longer chunks; elsewhere they are rounded to bf16, as in cascade_attn_sharded.
+ * So the last bits of a row depend on how many rows stand beside it.  fp32 operands are taken apart into two tf32 parts each, and
+ * products keep what lies above 2^-21 of themselves.
  *   workspace  cascade_attn_paged_workspace_bytes(...) bytes, 256-byte aligned; overwritten by every call, so calls that may run at
  *              the same time need one each
  * Errors: INVALID_ARG, UNSUPPORTED, WORKSPACE, CUDA.

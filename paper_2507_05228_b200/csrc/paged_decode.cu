@@ -10,8 +10,9 @@
 //   and 109, and from 5 rows on in tiles of 256 that are nearly empty 131.  4 sequences of 6 rows 52 -> 30.
 // The weights go into the second product as two bf16 parts, the upper 16 bits and the rest, so that they keep 16 bits of mantissa: the
 // loads are the limit, and with one part the rounding of few rows of weights was most of the error (2500 rows, 32 heads: 2.4e-3 of
-// the output, 1.7e-3 with two, which is its own rounding).  From 17 columns on the products are the limit: one part, rounded to nearest,
-// as in the tile kernel (16 sequences of 6 rows 108 -> 98 us, of 8 136 -> 119).
+// the output, 1.7e-3 with two, which is its own rounding).  From 17 columns on the products are a limit too: one part, rounded to
+// nearest, as in the tile kernel with heads of 128 (us, two parts | one: 16 sequences of 6 rows 80 | 82, of 8 89 | 83, 4 of 6 27 | 24; 16 of 6
+// with heads of 64 56 | 52).
 //
 // fp32 the same way with m16n8k8 products of operands cut into two tf32 parts (tf32.cuh); weights go from the lanes of their keys to
 // those of their columns by shuffles, and every block's products with the values are summed by themselves and added in fp32.

@@ -18,8 +18,8 @@
 // where sequences have them, 16 otherwise (16 in the example above: 40 us).  Where CTAs are few, key_parts of them share the keys and
 // leave partials, which paged_combine_kernel adds up.
 // What bounds it: half the time of the CTA with the longest keys is its products (12288 of 8 cycles, four at a time), a fifth the
-// chain of look-ups and first loads.  Long chunks take 12.9 cycles a product where the units take 8.3 (512 rows over 4000, 32 / 8 heads of
-// 128, 713 us; 327 at 96 TFLOP/s, a third of the rate of tf32).
+// chain of look-ups and first loads.  Long chunks take 13.2 cycles a product where the units take 8.3 (512 rows over 4000, 32 / 8 heads of
+// 128, 729 us; 327 at 96 TFLOP/s, a third of the rate of tf32).
 #include <algorithm>
 
 #include "paged.cuh"
@@ -428,7 +428,7 @@ cudaError_t launch_d(const AttnParams& p, cudaStream_t stream) {
 
 // Keys of a tile are shared by as many CTAs, at least 256 keys of what the table can hold each, as make the rounds of a CTA per SM and the keys
 // of a CTA, with 256 for its start and its end, come out shortest.  (us, as many CTAs as fit in one round | so: 299 rows over 3725, 16 / 8
-// heads of 128, 80 tiles: 358 | 243; 512 over 4000, 12 heads of 64, 96 tiles: 183 | 129.  The 256, us, two CTAs per SM and 512 keys | one and
+// heads of 128, 80 tiles: 358 | 247; 512 over 4000, 12 heads of 64, 96 tiles: 183 | 130.  The 256, us, two CTAs per SM and 512 keys | one and
 // 256: 3 drafts of 2 to 6 rows over 646 to 672, 32 / 8 heads of 128, 37 | 25; 28 over 4000, 12 heads of 128, 64 | 44.)
 int paged_f32_parts(const AttnParams& p) {
   const int64_t ctas = tiles_bound(p, wide(p) ? 64 : 16) * (p.H >> heads_log2(p.G)), keys = (int64_t)p.paged.max_pages * p.paged.page_size;
