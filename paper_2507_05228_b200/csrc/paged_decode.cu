@@ -1060,10 +1060,19 @@ __global__ void __launch_bounds__(kRangeThreads, kHalfCtas<T, D, NT>)
     }
     left -= s1 - s0;
     s0 = 0;
-    if (++item == a.items) {  // the next sequence that has blocks
+    if (left == 0) break;
+    if (++item == a.items) {  // the next sequence that has blocks; there may be many idle places before it
       item = 0;
-      do ++b;
-      while (b < g.batch && (blocks = blocks_of(g, b)) == 0);
+      for (++b; b < g.batch; b += 32) {
+        const int n = b + lane < g.batch ? blocks_of(g, b + lane) : 0;
+        const uint32_t some = __ballot_sync(0xffffffffu, n > 0);
+        if (some) {
+          const int who = __ffs(some) - 1;
+          blocks = __shfl_sync(0xffffffffu, n, who);
+          b += who;
+          break;
+        }
+      }
       if (b >= g.batch) break;
     }
     __syncthreads();  // the shares and queries have been read

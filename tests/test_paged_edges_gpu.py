@@ -162,3 +162,19 @@ def test_a_workspace_is_no_longer_than_its_memory():
         with pytest.raises(cb.CascadeError, match="workspace"):
             cb.cascade_attn_paged(b.q, b.k_pages, b.v_pages, b.table, b.row_start, b.kv_len, b.scale, max_rows=1, workspace=view)
     attend(b, max_rows=1, workspace=torch.zeros((1 << 13, 2 << 13), dtype=torch.uint8, device="cuda")[:, ::2])
+
+
+@pytest.mark.parametrize("dtype,d", [(torch.bfloat16, 128), (torch.bfloat16, 64), (torch.float32, 64)])
+@pytest.mark.parametrize("where", ["front", "ends", "spread"])
+@pytest.mark.parametrize("places,rows", [(70, 1), (3000, 1), (3000, 4), (8192, 1), (70, 20), (3000, 20)])
+def test_a_batch_of_idle_places(dtype, d, where, places, rows):
+    """Places of a cache that nobody has taken: no rows and no length."""
+    live = 50
+    at = {"front": list(range(live)), "ends": list(range(live // 2)) + list(range(places - live // 2, places)),
+          "spread": [i * (places - 1) // (live - 1) for i in range(live)]}[where]
+    rng = np.random.default_rng(places)
+    news, lens = [0] * places, [0] * places
+    for i in at:
+        news[i], lens[i] = int(rng.integers(1, rows + 1)), int(rng.integers(rows, 400))
+    b = pu.Batch(news, lens, 8, 2, d, 16, dtype, seed=rows, width=200)
+    attend(b, max_rows=rows)
