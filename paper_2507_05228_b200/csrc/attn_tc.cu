@@ -1717,7 +1717,10 @@ cudaError_t launch_paged_tc(const AttnParams& p, int max_rows, cudaStream_t stre
   const int64_t per = 256 >> lg, few = p.paged.least - 1, over = std::max<int64_t>(0, g.n_rows - g.batch * few);
   const int64_t seqs = (over + std::max<int64_t>(1, max_rows - few) - 1) / std::max<int64_t>(1, max_rows - few);
   const int64_t least = std::max((g.n_rows + per - 1) / per, std::min<int64_t>(g.batch, seqs));
-  const int64_t bound = g.batch == 1 ? (g.n_rows + per - 1) / per : std::min<int64_t>(g.n_rows, g.n_rows / per + g.batch);
+  // The grid has a CTA for every tile there could be: of the sequences that have g.least rows or more, no more than the rows make.  (us, 32 / 8
+  // heads of 128, 200 tokens over 200 to 2000 rows and 300 rows over 1200, with one of every sequence | so: 256 | 229; 64 of 8192 places with 20
+  // rows each, 8 / 2 heads of 64, 1760 | 239.)
+  const int64_t bound = g.batch == 1 ? (g.n_rows + per - 1) / per : std::min<int64_t>(g.n_rows, g.n_rows / per + std::min<int64_t>(g.batch, g.n_rows / g.least));
   const int64_t heads = p.H >> lg, key_tiles = ((int64_t)g.max_pages * g.page_size + 127) / 128;
   int lg_split = 0;  // as launch_attn_tc, by the keys that the table can hold
   const int64_t fit[4] = {148, 148, 132, 120};
@@ -1727,8 +1730,8 @@ cudaError_t launch_paged_tc(const AttnParams& p, int max_rows, cudaStream_t stre
   // 129 | 89, 4 of them 48 | 39; 35 rows over 7432, 16 / 8 heads, 27 | 24).  As a kernel of its own: where tiles are full the choice costs
   // them a hundredth (16 sequences of 1 to 701 rows, heads of 64, 98.0 -> 99.3).
   const bool twofold = std::min<int64_t>(max_rows, g.n_rows) << lg <= 128;
-  // `bound` counts a tile of every sequence and `least` of the few that must have one, so there can be clusters where the first is large (200
-  // single tokens and one chunk).  The CTAs of a cluster share a tile, which has to be on the slowest axis for that; it has room: with
+  // `bound` counts the tiles there could be and `least` those there must be, so there can be clusters where the first is large (200 single
+  // tokens and one chunk).  The CTAs of a cluster share a tile, which has to be on the slowest axis for that; it has room: with
   // clusters there are at most 74 tiles' rows in all, 256 each.
   const bool tile_major = lg_split > 0 || bound * heads <= 8 * (int64_t)sm_count();
   const TcLaunch l = {lg, tile_major, lg_split, 0, false, false, true, twofold};

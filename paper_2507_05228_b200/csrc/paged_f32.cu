@@ -395,10 +395,10 @@ int heads_log2(int G) {  // heads of a tile: as many of the G as a power of two 
   while (lg < 3 && G % (2 << lg) == 0) ++lg;
   return lg;
 }
-// Tiles of `height` (token, head) rows: every sequence can end in one that is not full.
+// Tiles of `height` (token, head) rows: every sequence that has rows can end in one that is not full.
 int64_t tiles_bound(const AttnParams& p, int height) {
   const int per = height >> heads_log2(p.G);
-  return p.paged.batch == 1 ? (p.paged.n_rows + per - 1) / per : p.paged.n_rows / per + p.paged.batch;
+  return p.paged.batch == 1 ? (p.paged.n_rows + per - 1) / per : p.paged.n_rows / per + std::min(p.paged.batch, p.paged.n_rows);
 }
 // Sixty-four rows a CTA where a sequence has half of them on average
 bool wide(const AttnParams& p) { return (p.paged.n_rows / p.paged.batch) << heads_log2(p.G) >= 32; }
